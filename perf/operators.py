@@ -1,0 +1,463 @@
+"""Performance cases of the rollout operators: what an actor runs between two transitions of its weights.
+
+Generation keeps keys and values in a paged cache: every step appends the new tokens' keys and values
+(with the position rotation applied on the way) and attends over them, the samples of one prompt sharing the pages of
+that prompt.  Scoring turns logits into the log probability of the given tokens, the entropy and the top
+alternatives; training takes the gradient of the first two back to the logits.
+
+Heads, widths and vocabularies are those of the benchmark's models and of their generation TP slices (the 70B shape over
+four ranks has 16 query and 2 KV heads), or the tests' odd ones.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+NEVER = -100  # a target that marks a position without one (prompt tokens, padding)
+
+
+def _append(name, dtype, heads, tokens, page, by="heads", rot=None, interleaved=False, fused=False, table=8192):
+    c = dict(op="append", dtype=dtype, q_heads=heads[0], kv_heads=heads[1], head_dim=heads[2], tokens=tokens, page=page, by=by,
+             rot=heads[2] if rot is None else rot, interleaved=interleaved, fused=fused, table=table)
+    return dict(c, name=name) if name else c
+
+
+def _attend(name, dtype, heads, prompts, samples, prefix, suffix, page, by="heads", ragged=False):
+    c = dict(op="attend", dtype=dtype, q_heads=heads[0], kv_heads=heads[1], head_dim=heads[2], prompts=prompts, samples=samples,
+             prefix=prefix, suffix=suffix, page=page, by=by, ragged=ragged)
+    return dict(c, name=name) if name else c
+
+
+def _score(name, dtype, rows, vocab, top, without=0.0, temperature=1.0):
+    c = dict(op="score", dtype=dtype, rows=rows, vocab=vocab, top=top, without=without, temperature=temperature)
+    return dict(c, name=name) if name else c
+
+
+def _train(name, dtype, rows, vocab, without=0.0, temperature=1.0, pad=0):
+    c = dict(op="train", dtype=dtype, rows=rows, vocab=vocab, without=without, temperature=temperature, pad=pad)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one sequence's next token at the 7B shape: bound by the launch
+        _append("append_one", "bf16", (32, 32, 128), 1, 64),
+        # one step of 256 sequences on one of four ranks of the 70B shape
+        _append("append_step", "bf16", (16, 2, 128), 256, 64),
+        # sixteen prompts of 512 tokens at the 7B shape, q, k and v out of one projection, pages of 16 with the tokens outside
+        _append("append_prompts", "bf16", (32, 32, 128), 8192, 16, by="tokens", fused=True),
+        # one step of the tiny decoder: four samples of a short prompt, bound by latency
+        _attend("attend_tiny", "bf16", (4, 4, 64), 1, 4, 100, 64, 16),
+        # the 7B shape (a KV head per query head): 16 prompts, eight samples each, half way through their responses
+        _attend("attend_7b", "bf16", (32, 32, 128), 16, 8, 1024, 1024, 64),
+        # the 70B shape on one GPU (eight query heads to a KV head): 8 prompts, 16 samples each
+        _attend("attend_70b", "bf16", (64, 8, 128), 8, 16, 2048, 2048, 64),
+        # 64 samples of one very long prompt on one of four ranks of the 70B shape; odd lengths, pages of 16 with the tokens outside
+        _attend("attend_long", "f16", (16, 2, 128), 1, 61, 32749, 509, 16, by="tokens", ragged=True),
+        # one step of 64 sequences, their sampled tokens' log probabilities with five alternatives
+        _score("score_step", "bf16", 64, 32000, 5),
+        # reference log probabilities of a micro-batch, a third of it prompt tokens without a target; no alternatives
+        _score("score_micro_batch", "bf16", 4096, 32000, 0, without=0.33, temperature=0.7),
+        # the 70B shape's vocabulary in 32 bits with twenty alternatives
+        _score("score_large", "f32", 2048, 128256, 20),
+        # the actor's update at the 7B shape: forward, then the gradients of log probability and entropy
+        _train("train_7b", "bf16", 4096, 32000, without=0.33),
+        # an odd batch over the tests' odd vocabulary, rows one element apart from their alignment
+        _train("train_odd", "f16", 1361, 5004, without=0.2, temperature=0.9, pad=1),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["append", "attend", "attend", "score", "train"])
+    heads = rng.choice([(32, 32, 128), (20, 20, 128), (64, 8, 128), (16, 2, 128), (12, 12, 64), (16, 8, 32), (8, 4, 72)])
+    half = rng.choice(["bf16", "bf16", "f16"])
+    by = rng.choice(["heads", "heads", "tokens"])
+    page = rng.choice([8, 16, 32, 64, 128])
+    if op == "append":
+        rot = rng.choice([heads[2], heads[2], heads[2] // 2])
+        tokens = min(_log_uniform(rng, 1, 8192), (256 << 20) // (2 * heads[2] * (heads[0] + 2 * heads[1])))
+        return _append("", half, heads, tokens, page, by, rot, rng.random() < 0.3, rng.random() < 0.5)
+    if op == "attend":
+        prompts, samples = _log_uniform(rng, 1, 32), _log_uniform(rng, 1, 64)
+        prefix, suffix = _log_uniform(rng, 1, 32768), _log_uniform(rng, 1, 4096)
+        token = 4 * heads[1] * heads[2]
+        seen = lambda: 4 * prompts * samples * (prefix + suffix // 2) * heads[0] * heads[2]  # noqa: E731
+        while prompts * (prefix + samples * suffix // 2) * token > 1 << 30 or seen() > 12e9:
+            prompts, samples, suffix = max(1, prompts // 2), max(1, samples - samples // 4), max(1, suffix - suffix // 4)
+            prefix = max(1, prefix - prefix // 8)
+        return _attend("", half, heads, prompts, samples, prefix, suffix, page, by, rng.random() < 0.5)
+    dtype = rng.choice(["bf16", "bf16", "f16", "f32"])
+    vocab = rng.choice([1024, 5004, 32000, 32000, 50257, 128256, _log_uniform(rng, 100, 130000)])
+    size = 4 if dtype == "f32" else 2
+    rows = min(_log_uniform(rng, 1, 8192), (1 << 29) // (size * vocab))
+    without, temperature = rng.choice([0.0, 0.33, 0.5]), rng.choice([1.0, 1.0, 0.7, 1.3])
+    if op == "score":
+        return _score("", dtype, rows, vocab, rng.choice([0, 1, 5, 20]), without, temperature)
+    return _train("", dtype, rows // 2 + 1, vocab, without, temperature, rng.choice([0, 0, 1, 8]))
+
+
+# ---- what lengths a case has: by the case alone, the seed only deals them out --------------------------------------------
+
+def _group_sizes(c):
+    """Samples of each prompt: all of them, or fewer where some are done."""
+    if not c["ragged"]:
+        return [c["samples"]] * c["prompts"]
+    return [max(1, c["samples"] - (g * 5) % (c["samples"] // 2 + 1)) for g in range(c["prompts"])]
+
+
+def _prefix_lens(c):
+    """From half the longest prompt up to it."""
+    return [c["prefix"] - (g * 77) % (c["prefix"] // 2 + 1) for g in range(c["prompts"])]
+
+
+def _suffix_lens(c, n):
+    """Evenly from one token to the longest response."""
+    return [1 + ((c["suffix"] - 1) * (i + 1)) // n for i in range(n)]
+
+
+def _without(c):
+    return int(c["rows"] * c["without"])
+
+
+# ---- inputs --------------------------------------------------------------------------------------------------------------
+
+def _cache(c, pages, gen, dtype):
+    """Keys and values as [page, KV head, token, element], in either order of memory."""
+    h, p, d = c["kv_heads"], c["page"], c["head_dim"]
+    shape = (pages, h, p, d) if c["by"] == "heads" else (pages, p, h, d)
+    made = [torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32).to(dtype) for _ in range(2)]
+    return made if c["by"] == "heads" else [t.transpose(1, 2) for t in made]
+
+
+def _prepare_append(c, gen, dtype):
+    t, hq, hk, d = c["tokens"], c["q_heads"], c["kv_heads"], c["head_dim"]
+    s = {}
+    if c["fused"]:
+        x = torch.randn(t, (hq + 2 * hk) * d, generator=gen, device="cuda").to(dtype)
+        s["q"], s["k"], s["v"] = (y.view(t, -1, d) for y in x.split([hq * d, hk * d, hk * d], 1))
+    else:
+        for n, h in (("q", hq), ("k", hk), ("v", hk)):
+            s[n] = torch.randn(t, h, d, generator=gen, device="cuda").to(dtype)
+    s["q_out"] = torch.zeros(t, hq, d, device="cuda", dtype=dtype)
+    pages = -(-t // c["page"]) + 3
+    s["cache_k"], s["cache_v"] = _cache(c, pages, gen, dtype)
+    s["slots"] = torch.randperm(pages * c["page"], generator=gen, device="cuda")[:t].contiguous()
+    if t > 16:
+        s["slots"][5::16] = -1  # padding
+    s["positions"] = torch.randint(0, c["table"], (t,), generator=gen, device="cuda", dtype=torch.int32)
+    at = torch.arange(c["table"], device="cuda", dtype=torch.float64)[:, None]
+    at = at * 10000.0 ** (-torch.arange(0, c["rot"], 2, device="cuda", dtype=torch.float64) / c["rot"])
+    s["cos"], s["sin"] = at.cos().float(), at.sin().float()
+    return s
+
+
+def _table(lens, page, at):
+    """Page tables: every row its own pages, dealt out of `at` (a permutation); unused entries -1."""
+    width = max(-(-n // page) for n in lens)
+    need = torch.tensor([-(-n // page) for n in lens])
+    begin = torch.cumsum(need, 0) - need
+    i = torch.arange(width)[None, :]
+    where = (begin[:, None] + i).clamp(max=at.numel() - 1).cuda()
+    return torch.where((i < need[:, None]).cuda(), at[where], -1).to(torch.int32).contiguous(), int(need.sum())
+
+
+def _prepare_attend(c, gen, dtype):
+    sizes, prefix = _group_sizes(c), _prefix_lens(c)
+    b = sum(sizes)
+    suffix = _suffix_lens(c, b)
+    deal = torch.randperm(b, generator=gen, device="cuda").cpu().tolist()
+    suffix = [suffix[i] for i in deal]
+    pages = sum(-(-n // c["page"]) for n in prefix + suffix)
+    s = {}
+    s["cache_k"], s["cache_v"] = _cache(c, pages, gen, dtype)
+    at = torch.randperm(pages, generator=gen, device="cuda")
+    s["prefix_pages"], used = _table(prefix, c["page"], at)
+    s["suffix_pages"], _ = _table(suffix, c["page"], at[used:])
+    s["prefix_lens"], s["suffix_lens"] = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (prefix, suffix))
+    offsets = [sum(sizes[:g]) for g in range(len(sizes) + 1)]
+    s["group_offsets"] = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    s["max_group"] = max(sizes)
+    s["q"] = (1.5 * torch.randn(b, c["q_heads"], c["head_dim"], generator=gen, device="cuda")).to(dtype)
+    s["scale"] = c["head_dim"] ** -0.5
+    return s
+
+
+def _prepare_logits(c, gen, dtype):
+    """Logits with the spread of a language model's, the given token mostly among the likely ones."""
+    r, v = c["rows"], c["vocab"]
+    width = v + c.get("pad", 0)
+    store = torch.empty(r, width, device="cuda", dtype=dtype)
+    for i in range(0, r, 512):
+        n = min(512, r - i)
+        store[i:i + n] = 2.2 * torch.randn(n, width, generator=gen, device="cuda")
+    logits = store[:, :v]
+    targets = torch.randint(0, v, (r,), generator=gen, device="cuda")
+    rows = torch.arange(r, device="cuda")
+    logits[rows, targets] += (9 * torch.rand(r, generator=gen, device="cuda") * (torch.rand(r, generator=gen, device="cuda") < 0.8)).to(dtype)
+    targets[torch.randperm(r, generator=gen, device="cuda")[:_without(c)]] = NEVER
+    s = dict(logits=logits, targets=targets, temperature=c["temperature"], top=c.get("top", 0))
+    if c["op"] == "train":
+        s["grad_logprob"] = torch.randn(r, generator=gen, device="cuda")
+        s["grad_entropy"] = 0.01 * torch.rand(r, generator=gen, device="cuda")
+    return s
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    make = {"append": _prepare_append, "attend": _prepare_attend}.get(case["op"], _prepare_logits)
+    s = make(case, gen, DTYPES[case["dtype"]])
+    s["op"], s["interleaved"] = case["op"], case.get("interleaved", False)
+    return s
+
+
+# ---- the plain forms -----------------------------------------------------------------------------------------------------
+
+def _rotate_plain(x, cos, sin, interleaved):
+    """[token, head, element] in 32 bits: the pairs turned by their angles, elements past the rotated ones as they are."""
+    n = cos.shape[1]
+    c, s = cos[:, None, :], sin[:, None, :]
+    a, b = (x[..., 0:2 * n:2], x[..., 1:2 * n:2]) if interleaved else (x[..., :n], x[..., n:2 * n])
+    u, w = a * c - b * s, b * c + a * s
+    turned = torch.stack((u, w), -1).flatten(-2) if interleaved else torch.cat((u, w), -1)
+    return torch.cat((turned, x[..., 2 * n:]), -1)
+
+
+def _append_plain(s):
+    t, page = s["slots"].shape[0], s["cache_k"].shape[2]
+    live = s["slots"] >= 0
+    # a token without a place repeats the first one that has one
+    src = torch.where(live, torch.arange(t, device=live.device), live.to(torch.int32).argmax())
+    pos, slot = s["positions"][src], s["slots"][src]
+    cos, sin = s["cos"][pos], s["sin"][pos]
+    turn = lambda x: _rotate_plain(x[src].float(), cos, sin, s["interleaved"]).to(x.dtype)  # noqa: E731
+    s["q_out"][src] = turn(s["q"])
+    s["cache_k"][slot // page, :, slot % page] = turn(s["k"])
+    s["cache_v"][slot // page, :, slot % page] = s["v"][src]
+    return {"q": s["q_out"], "k": s["cache_k"], "v": s["cache_v"]}
+
+
+def _tokens_plain(cache, table):
+    """[row, KV head, token, element] in 32 bits: the pages that a table names, one after another."""
+    x = cache[table.clamp(min=0).long()].float().transpose(1, 2)
+    return x.flatten(2, 3)
+
+
+def _attend_plain(s):
+    b, hq, d = s["q"].shape
+    hk = s["cache_k"].shape[1]
+    ratio, dev = hq // hk, s["q"].device
+    off = s["group_offsets"].long()
+    groups, most = off.numel() - 1, s["max_group"]
+    q = s["q"].float().view(b, hk, ratio, d) * s["scale"]
+    seq = torch.arange(b, device=dev)
+    group = (seq[:, None] >= off[None, 1:]).sum(1)
+    member = seq - off[group]
+    # the prompt: the queries of its samples against its keys, one product per prompt and KV head
+    k, v = _tokens_plain(s["cache_k"], s["prefix_pages"]), _tokens_plain(s["cache_v"], s["prefix_pages"])
+    rows = (off[:-1, None] + torch.arange(most, device=dev)).clamp(max=b - 1)
+    qs = q[rows].permute(0, 2, 1, 3, 4).reshape(groups, hk, most * ratio, d)
+    x = torch.matmul(qs, k.transpose(-1, -2))
+    seen = torch.arange(k.shape[2], device=dev) < s["prefix_lens"][:, None]
+    x = x.masked_fill(~seen[:, None, None], -math.inf)
+    mp = x.amax(-1, keepdim=True)
+    e = (x - mp).exp()
+    lp, op = e.sum(-1, keepdim=True), torch.matmul(e, v)
+    mp, lp, op = (y.view(groups, hk, most, ratio, -1)[group, :, member] for y in (mp, lp, op))
+    # the responses: every sequence's own keys
+    k, v = _tokens_plain(s["cache_k"], s["suffix_pages"]), _tokens_plain(s["cache_v"], s["suffix_pages"])
+    x = torch.matmul(q, k.transpose(-1, -2))
+    seen = torch.arange(k.shape[2], device=dev) < s["suffix_lens"][:, None]
+    x = x.masked_fill(~seen[:, None, None], -math.inf)
+    m = torch.maximum(x.amax(-1, keepdim=True), mp)
+    e = (x - m).exp()
+    l = e.sum(-1, keepdim=True) + lp * (mp - m).exp()
+    o = (torch.matmul(e, v) + op * (mp - m).exp()) / l
+    return {"out": o.reshape(b, hq, d).to(s["q"].dtype), "lse": (m + l.log()).reshape(b, hq)}
+
+
+def _softmax_plain(s):
+    """(logits over the temperature, log sum of their exponentials, entropy) in 32 bits; a row that is all -inf has no entropy."""
+    x = s["logits"].float() / s["temperature"]
+    m = x.amax(1, keepdim=True)
+    m = torch.where(m == -math.inf, 0.0, m)
+    d = x - m
+    e = d.exp()
+    z = e.sum(1, keepdim=True)
+    ent = torch.where(z > 0, z.log() - torch.where(e > 0, e * d, 0.0).sum(1, keepdim=True) / z, 0.0)
+    return x, m + z.log(), ent
+
+
+def _score_plain(s):
+    x, lse, ent = _softmax_plain(s)
+    live = (s["targets"] >= 0)[:, None]
+    at = s["targets"].clamp(min=0)[:, None]
+    out = {"logprob": torch.where(live, x.gather(1, at) - lse, 0.0)[:, 0], "entropy": torch.where(live, ent, 0.0)[:, 0]}
+    if s["top"]:
+        # value first, then the lower index: one key in 64 bits, the value's bits in the order of the values
+        bits = s["logits"].float().view(torch.int32)
+        order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).to(torch.int64)
+        key = (order << 32) | (0xFFFFFFFF - torch.arange(x.shape[1], device=x.device))
+        ids = 0xFFFFFFFF - (key.topk(s["top"], dim=1).values & 0xFFFFFFFF)
+        out["top_ids"] = torch.where(live, ids, -1).to(torch.int32)
+        out["top_logprobs"] = torch.where(live, x.gather(1, ids) - lse, 0.0)
+    return out
+
+
+def _train_plain(s):
+    x, lse, ent = _softmax_plain(s)
+    live = (s["targets"] >= 0)[:, None]
+    at = s["targets"].clamp(min=0)[:, None]
+    logp = x - lse
+    p = logp.exp()
+    g, h = s["grad_logprob"][:, None], s["grad_entropy"][:, None]
+    grad = -p * (g + h * torch.where(p > 0, logp + ent, 0.0))
+    grad.scatter_add_(1, at, g)
+    grad = torch.where(live, grad / s["temperature"], 0.0).to(s["logits"].dtype)
+    return {"logprob": torch.where(live, logp.gather(1, at), 0.0)[:, 0], "entropy": torch.where(live, ent, 0.0)[:, 0], "grad": grad}
+
+
+# ---- the framework's operators -------------------------------------------------------------------------------------------
+
+def _run_own(s):
+    from paper_2409_19256_amd import rollout
+    if s["op"] in ("append", "attend") and "cache" not in s:
+        s["cache"] = rollout.KvCache(s["cache_k"], s["cache_v"])  # the handle that a program keeps beside its cache
+    if s["op"] == "append":
+        s["cache"].append(s["k"], s["v"], s["slots"], s["positions"], s["cos"], s["sin"], q=s["q"], q_out=s["q_out"],
+                          interleaved=s["interleaved"])
+        return {"q": s["q_out"], "k": s["cache_k"], "v": s["cache_v"]}
+    if s["op"] == "attend":
+        out, lse = s["cache"].attend(s["q"], s["suffix_lens"], s["suffix_pages"], s["group_offsets"], s["prefix_lens"],
+                                     s["prefix_pages"], max_group=s["max_group"], scale=s["scale"])
+        return {"out": out, "lse": lse}
+    r = rollout.token_logprobs(s["logits"], s["targets"], temperature=s["temperature"], top=s["top"])
+    out = {"logprob": r.logprob, "entropy": r.entropy}
+    if s["op"] == "train":
+        out["grad"] = rollout.token_logprobs_back(s["logits"], s["targets"], r.lse, r.entropy, s["grad_logprob"], s["grad_entropy"],
+                                                  temperature=s["temperature"])
+    elif s["top"]:
+        out["top_ids"], out["top_logprobs"] = r.top_ids, r.top_logprobs
+    return out
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"append": _append_plain, "attend": _attend_plain, "score": _score_plain, "train": _train_plain}[state["op"]](state)
+
+
+# ---- what a pass cannot do without ---------------------------------------------------------------------------------------
+
+def work(case):
+    c = case
+    size = 4 if c["dtype"] == "f32" else 2
+    if c["op"] == "append":
+        t = c["tokens"] - (len(range(5, c["tokens"], 16)) if c["tokens"] > 16 else 0)
+        heads = c["q_heads"] + 2 * c["kv_heads"]
+        return {"bytes": t * (2 * size * heads * c["head_dim"] + 12 + 4 * c["rot"]), "flops": 3 * t * (c["q_heads"] + c["kv_heads"]) * c["rot"]}
+    if c["op"] == "attend":
+        sizes, prefix = _group_sizes(c), _prefix_lens(c)
+        b = sum(sizes)
+        suffix = sum(_suffix_lens(c, b))
+        read = 2 * size * c["kv_heads"] * c["head_dim"] * (sum(prefix) + suffix)
+        read += 4 * sum(-(-n // c["page"]) for n in prefix + _suffix_lens(c, b))
+        seen = suffix + sum(n * m for n, m in zip(sizes, prefix))
+        return {"bytes": read + b * c["q_heads"] * (2 * size * c["head_dim"] + 4), "flops": 4 * seen * c["q_heads"] * c["head_dim"]}
+    rows, live = c["rows"], c["rows"] - _without(c)
+    n = live * c["vocab"]
+    if c["op"] == "score":
+        return {"bytes": n * size + rows * (16 + 8 * c["top"]), "flops": 5 * n}
+    # the softmax has to be whole before the first gradient: read, then written
+    return {"bytes": n * size + rows * c["vocab"] * size + rows * 24, "flops": 10 * n}
+
+
+# ---- 64 bits -------------------------------------------------------------------------------------------------------------
+
+def _exact_append(s):
+    rot = 2 * s["cos"].shape[1]
+    half = rot // 2
+    if s["interleaved"]:
+        first = torch.arange(0, rot, 2, device="cuda")
+        second = first + 1
+    else:
+        first = torch.arange(half, device="cuda")
+        second = first + half
+    live = (s["slots"] >= 0).nonzero()[:, 0]
+    angle = s["positions"][live].long()
+    cos, sin = s["cos"].double()[angle][:, None], s["sin"].double()[angle][:, None]
+    out = {"q": s["q_out"].double(), "k": s["cache_k"].double(), "v": s["cache_v"].double()}
+    page = s["cache_k"].shape[2]
+    at, inside = s["slots"][live] // page, s["slots"][live] % page
+    for name, x in (("q", s["q"]), ("k", s["k"])):
+        y = x[live].double()
+        z = y.clone()
+        z[..., first] = y[..., first] * cos - y[..., second] * sin
+        z[..., second] = y[..., first] * sin + y[..., second] * cos
+        if name == "q":
+            out["q"][live] = z
+        else:
+            out["k"][at, :, inside] = z
+    out["v"][at, :, inside] = s["v"][live].double()
+    return out
+
+
+def _exact_attend(s):
+    """One sequence after another over all of its keys, the prompt's and its own."""
+    b, hq, d = s["q"].shape
+    hk = s["cache_k"].shape[1]
+    out = torch.empty(b, hq, d, device="cuda", dtype=torch.float64)
+    lse = torch.empty(b, hq, device="cuda", dtype=torch.float64)
+    off, plen, slen = (s[n].tolist() for n in ("group_offsets", "prefix_lens", "suffix_lens"))
+
+    def keys(table, n):
+        return [c[table.long()[:-(-n // c.shape[2])]].double().transpose(0, 1).reshape(hk, -1, d)[:, :n] for c in (s["cache_k"], s["cache_v"])]
+
+    for g in range(len(plen)):
+        pk, pv = keys(s["prefix_pages"][g], plen[g])
+        for i in range(off[g], off[g + 1]):
+            sk, sv = keys(s["suffix_pages"][i], slen[i])
+            k, v = torch.cat((pk, sk), 1), torch.cat((pv, sv), 1)
+            x = (torch.bmm(s["q"][i].double().view(hk, hq // hk, d), k.transpose(1, 2).contiguous()) * s["scale"])
+            lse[i] = torch.logsumexp(x, -1).reshape(hq)
+            out[i] = torch.bmm(torch.softmax(x, -1), v).reshape(hq, d)
+    return {"out": out, "lse": lse}
+
+
+def _exact_logits(s, train):
+    r = s["logits"].shape[0]
+    got = {"logprob": torch.zeros(r, device="cuda", dtype=torch.float64), "entropy": torch.zeros(r, device="cuda", dtype=torch.float64)}
+    if train:
+        got["grad"] = torch.zeros(s["logits"].shape, device="cuda", dtype=torch.float64)
+    elif s["top"]:
+        got["top_ids"], got["top_logprobs"] = None, torch.zeros(r, s["top"], device="cuda", dtype=torch.float64)
+    live = (s["targets"] >= 0).nonzero()[:, 0]
+    for rows in live.split(256):
+        x = s["logits"][rows].double() / s["temperature"]
+        logp = torch.log_softmax(x, 1)
+        p = logp.exp()
+        t = s["targets"][rows]
+        got["logprob"][rows] = logp[torch.arange(len(rows), device="cuda"), t]
+        ent = -torch.special.xlogy(p, p).sum(1)
+        got["entropy"][rows] = ent
+        if train:
+            g, h = s["grad_logprob"][rows].double()[:, None], s["grad_entropy"][rows].double()[:, None]
+            hot = torch.nn.functional.one_hot(t, x.shape[1])
+            got["grad"][rows] = (g * (hot - p) - h * (torch.special.xlogy(p, p) + p * ent[:, None])) / s["temperature"]
+        elif s["top"]:
+            got["top_logprobs"][rows] = logp.topk(s["top"], 1).values
+    return got
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "append":
+        return _exact_append(s)
+    if case["op"] == "attend":
+        return _exact_attend(s)
+    return _exact_logits(s, case["op"] == "train")
