@@ -339,7 +339,7 @@ def _run_own(s):
     r = rollout.token_logprobs(s["logits"], s["targets"], temperature=s["temperature"], top=s["top"])
     out = {"logprob": r.logprob, "entropy": r.entropy}
     if s["op"] == "train":
-        out["grad"] = rollout.token_logprobs_back(s["logits"], s["targets"], r.lse, r.entropy, s["grad_logprob"], s["grad_entropy"],
+        out["grad"] = rollout.token_logprobs_back(s["logits"], s["targets"], r.norm, r.entropy, s["grad_logprob"], s["grad_entropy"],
                                                   temperature=s["temperature"])
     elif s["top"]:
         out["top_ids"], out["top_logprobs"] = r.top_ids, r.top_logprobs
