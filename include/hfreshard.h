@@ -487,6 +487,136 @@ HF_API int hf_plan_get_tile_dst(const hf_plan *plan, int direction, size_t i, ui
  * shared copy records of their block and stay inside their rows.  O(bytes/row) time: meant for tests, not for the hot path. */
 HF_API int hf_plan_validate(const hf_plan *plan);
 
+/* ---- rollout operators ---------------------------------------------------------------
+ * What the actor runs between two transitions of its weights: generation appends the new tokens' keys and values to
+ * a paged cache and attends over it, the samples of one prompt sharing that prompt's pages (Section 5.2 step 2);
+ * scoring and the update take log probabilities of given tokens out of the logits, and their gradient back
+ * (compute_log_prob and compute_loss of Section 4).
+ * Conventions: all pointers inside the argument structs are DEVICE pointers of the current HIP device, the structs
+ * themselves are host memory and are read before the call returns.  Strides count ELEMENTS, are not negative, and the last
+ * dimension is contiguous; data are aligned to their element, everything else to 4 bytes (64-bit integers to 8).  The calls enqueue one or two
+ * kernels on hip_stream and return; they never allocate, synchronise or keep anything from one call for the next, so
+ * they can be captured into a graph.  Lengths, page numbers, slots, positions and targets are read on the device: an
+ * entry outside its range is left out as said below and never leads to an access outside the buffers.  Sums, softmax
+ * statistics and rotations are held in 32 bits and rounded once to the type of the output.  Results do not depend
+ * on what else runs: nothing is added up by atomics.  HF_EINVAL: null pointer, unknown type or flag, size or stride out of contract,
+ * output that overlaps itself or an input; HF_ERANGE: a call that does not fit one HIP grid. */
+enum { HF_BF16 = 0, HF_F16 = 1, HF_F32 = 2 }; /* element types */
+
+/* A paged cache of keys and values.  Element (page, head, token, i) of either is at
+ * page * page_stride + head * head_stride + token * token_stride + i, so that the heads may lie outside the tokens of a
+ * page (the faster order for attention: a page of one head is read in one piece) or inside.  64-bit offsets throughout. */
+typedef struct {
+  void *k, *v;
+  int32_t dtype;       /* HF_BF16 or HF_F16 */
+  int32_t n_kv_heads, head_dim; /* head_dim 1 .. 256; multiples of 8 with strides to match move 16 bytes at a time */
+  int32_t page_tokens; /* power of two, 4 .. 65536 */
+  int64_t n_pages;     /* 1 .. 2^31 - 1 */
+  int64_t page_stride, head_stride, token_stride;
+} hf_kv_cache;
+
+#define HF_ROT_INTERLEAVED 0x1u /* the pairs are (2i, 2i+1); without it (i, i + rot_dim / 2) */
+
+/* hf_append_kv: keys and values of n_tokens new tokens go to their places in the cache, the keys with the position
+ * rotation applied; q, if given, is rotated the same way into q_out (which may be q itself, with the same strides).
+ * Pair i of a head at position p: (a, b) -> (a cos - b sin, b cos + a sin) with cos[p, i] and sin[p, i]; elements from
+ * rot_dim on are copied.  slots[t] = page * page_tokens + token inside the page; a token whose slot is negative (padding)
+ * or past the cache, or whose position is outside the table, is left out: nothing is written for it, q_out included.  No two tokens of a call may
+ * have the same slot.  One launch. */
+typedef struct {
+  const void *q;            /* [n_tokens, n_q_heads, head_dim], the cache's type; may be null */
+  void *q_out;              /* null exactly if q is */
+  const void *k, *v;        /* [n_tokens, n_kv_heads, head_dim] */
+  const float *cos, *sin;   /* [n_positions, rot_dim / 2], contiguous; null if rot_dim is 0 */
+  const int32_t *positions; /* [n_tokens]; null if rot_dim is 0 */
+  const int64_t *slots;     /* [n_tokens] */
+  int64_t q_stride, q_head_stride, q_out_stride, q_out_head_stride, k_stride, k_head_stride, v_stride, v_head_stride;
+  int32_t n_tokens, n_q_heads;
+  int32_t rot_dim, n_positions; /* rot_dim even, 0 .. head_dim */
+  uint32_t flags;
+  int32_t _pad;
+} hf_append;
+HF_API int hf_append_kv(const hf_kv_cache *cache, const hf_append *args, void *hip_stream);
+
+/* hf_attend: attention of one query token per sequence over its prompt's tokens and its own.  Sequences
+ * group_offsets[g] .. group_offsets[g+1]-1 are the samples of prompt g; their queries are taken together over the pages
+ * of the prompt, whose keys and values are read once for all of them.  Then every sequence's own pages (its response, the
+ * current token included) follow.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   x_j = scale * <q, k_j> over all visible tokens j;  out = sum_j exp(x_j - lse) v_j;  lse = log sum_j exp(x_j).
+ * A sequence without any visible token has out = 0 and lse = -inf.  Tokens past a length or on a page number
+ * outside the cache are not visible, whatever the cache holds there, NaN included; lengths are cut to the table's
+ * width * page_tokens and to max_prefix / max_suffix, below 0 they count as 0.  A sequence in no group has no prompt, and so have the
+ * members of a group past max_group.  A prompt may have any number of samples, a prompt processed by
+ * itself is a sequence per token with lengths 1, 2, 3, ... over one table row.
+ * workspace: at least hf_attend_workspace_bytes(cache, args) bytes, 16-byte aligned; its contents do not matter and are
+ * not kept.  One or two launches. */
+typedef struct {
+  const void *q; /* [n_seqs, n_q_heads, head_dim], the cache's type */
+  void *out;     /* the same shape and type; not q */
+  float *lse;    /* [n_seqs, n_q_heads], contiguous, natural logarithm; may be null */
+  const int32_t *suffix_lens;   /* [n_seqs] */
+  const int32_t *suffix_pages;  /* [n_seqs, suffix_width], contiguous */
+  const int32_t *group_offsets; /* [n_groups + 1], ascending */
+  const int32_t *prefix_lens;   /* [n_groups] */
+  const int32_t *prefix_pages;  /* [n_groups, prefix_width], contiguous */
+  void *workspace;
+  size_t workspace_bytes;
+  int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+  int32_t n_seqs, n_q_heads; /* n_q_heads a multiple of n_kv_heads */
+  int32_t n_groups;          /* 0: no prompts, the pointers to them may be null */
+  int32_t max_group;         /* most samples of a prompt */
+  int32_t prefix_width, suffix_width; /* pages per table row */
+  int32_t max_prefix, max_suffix;     /* upper bounds of the lengths: they shape the launch, so tight ones are faster */
+  float scale;
+  int32_t _pad;
+} hf_attention;
+HF_API size_t hf_attend_workspace_bytes(const hf_kv_cache *cache, const hf_attention *args); /* (size_t)-1: see hf_last_error */
+HF_API int hf_attend(const hf_kv_cache *cache, const hf_attention *args, void *hip_stream);
+
+/* Rows of logits with a given token each: y = x * inv_temperature. */
+typedef struct {
+  const void *logits;  /* [rows, vocab] of dtype, rows row_stride elements apart */
+  const void *targets; /* [rows] of int32 or int64 token ids; may be null (alternatives and entropy alone) */
+  int64_t rows, row_stride;
+  int32_t dtype;        /* HF_BF16, HF_F16 or HF_F32 */
+  int32_t vocab;        /* 1 .. 2^30 */
+  int32_t target_bytes; /* 4 or 8 */
+  float inv_temperature; /* > 0, finite */
+} hf_logits;
+
+#define HF_MAX_TOP 64
+/* hf_token_logprobs, for every row in one pass over it:
+ *   lse = log sum_j exp(y_j), logprob = y_target - lse, entropy = -sum_j p_j log p_j with p_j = exp(y_j - lse), and the top_n likeliest
+ *   tokens with their log probabilities, likeliest first, equal ones by the lower id.  norm holds lse in two parts, the largest logit x_max and
+ *   n = log sum_j exp((x_j - x_max) * inv_temperature), from which log p_j = (x_j - x_max) * inv_temperature - n comes out
+ *   whole where lse itself is rounded coarsely (a row masked with the type's lowest value).
+ * A row whose target is outside 0 .. vocab-1 (prompt tokens, padding) is not read: zeros, and ids of -1.  A logit of -inf (a token
+ * that is ruled out) has p = 0; a row of nothing else has lse, norm and log probabilities of -inf and entropy 0.  A row with NaN
+ * or +inf has NaN results, its ids are then any distinct ones.  Every output may be null.  One launch. */
+typedef struct {
+  float *logprob, *entropy, *lse; /* [rows] */
+  float *norm;                    /* [rows, 2], contiguous; what hf_token_logprobs_back wants */
+  int32_t *top_ids;               /* [rows, top_n], contiguous */
+  float *top_logprobs;            /* [rows, top_n], contiguous */
+  int32_t top_n;                  /* 0 .. min(vocab, HF_MAX_TOP) */
+  int32_t _pad;
+} hf_logprobs;
+HF_API int hf_token_logprobs(const hf_logits *in, const hf_logprobs *out, void *hip_stream);
+
+/* hf_token_logprobs_back: the gradient of sum_r (grad_logprob[r] * logprob[r] + grad_entropy[r] * entropy[r]),
+ *   dx_j = inv_temperature * (grad_logprob * ([j = target] - p_j) - grad_entropy * p_j * (log p_j + entropy)),
+ * from the norm and entropy that hf_token_logprobs gave for the same logits, temperature and targets.  p_j = 0 adds nothing (a row of -inf alone
+ * keeps grad_logprob at its target).  Rows without a target are set to 0, unread.  dlogits has the logits' type and may be the logits themselves, with the same
+ * stride.  One launch. */
+typedef struct {
+  const float *norm;                        /* [rows, 2], contiguous */
+  const float *entropy;                     /* [rows]; may be null if grad_entropy is */
+  const float *grad_logprob, *grad_entropy; /* [rows]; null = 0 */
+  void *dlogits;                            /* [rows, vocab] */
+  int64_t dlogits_stride;
+} hf_logprobs_grad;
+HF_API int hf_token_logprobs_back(const hf_logits *in, const hf_logprobs_grad *grad, void *hip_stream);
+
 HF_API const char *hf_last_error(void);
 HF_API const char *hf_version(void);
 

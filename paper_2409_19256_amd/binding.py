@@ -44,6 +44,9 @@ HF_MULTICAST_OFF, HF_MULTICAST_REGISTERS, HF_MULTICAST_CACHE_BLOCKED, HF_MULTICA
 HF_STATIC_SCRATCH_BYTES = 16 << 20
 HF_FANOUT_REGISTERS, HF_FANOUT_CACHE_BLOCKED, HF_FANOUT_PREFETCHED = 0, 1, 2
 HF_VARIANT_PERSISTENT, HF_VARIANT_ONE_WG_PER_TILE, HF_VARIANT_LDS_STAGED, HF_VARIANT_WAVE_PERSISTENT, HF_VARIANT_PARTS = 0, 1, 2, 3, 4
+HF_BF16, HF_F16, HF_F32 = 0, 1, 2
+HF_ROT_INTERLEAVED = 0x1
+HF_MAX_TOP = 64
 
 TENSOR_NAMES = {
     HF_T_EMBED: "embed", HF_T_LN1: "ln1", HF_T_QKV: "qkv", HF_T_O: "o", HF_T_LN2: "ln2", HF_T_GATE_UP: "gate_up",
@@ -84,6 +87,41 @@ class hf_tile(C.Structure):
     _fields_ = [("src_off", C.c_uint64), ("dst_off", C.c_uint64), ("rows", C.c_uint32), ("row_bytes", C.c_uint32),
                 ("src_row_stride", C.c_uint32), ("dst_row_stride", C.c_uint32), ("vec_bytes", C.c_uint32),
                 ("n_dst", C.c_uint32), ("dst_list", C.c_uint32), ("_pad", C.c_uint32)]
+
+
+class hf_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_tokens", C.c_int32), ("n_pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("token_stride", C.c_int64)]
+
+
+class hf_append(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "q_out", "k", "v", "cos", "sin", "positions", "slots")] +
+                [(n, C.c_int64) for n in ("q_stride", "q_head_stride", "q_out_stride", "q_out_head_stride", "k_stride", "k_head_stride",
+                                          "v_stride", "v_head_stride")] +
+                [("n_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("rot_dim", C.c_int32), ("n_positions", C.c_int32),
+                 ("flags", C.c_uint32), ("_pad", C.c_int32)])
+
+
+class hf_attention(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "lse", "suffix_lens", "suffix_pages", "group_offsets", "prefix_lens", "prefix_pages",
+                                           "workspace")] + [("workspace_bytes", C.c_size_t)] +
+                [(n, C.c_int64) for n in ("q_stride", "q_head_stride", "out_stride", "out_head_stride")] +
+                [(n, C.c_int32) for n in ("n_seqs", "n_q_heads", "n_groups", "max_group", "prefix_width", "suffix_width", "max_prefix",
+                                          "max_suffix")] + [("scale", C.c_float), ("_pad", C.c_int32)])
+
+
+class hf_logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("targets", C.c_void_p), ("rows", C.c_int64), ("row_stride", C.c_int64), ("dtype", C.c_int32),
+                ("vocab", C.c_int32), ("target_bytes", C.c_int32), ("inv_temperature", C.c_float)]
+
+
+class hf_logprobs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logprob", "entropy", "lse", "norm", "top_ids", "top_logprobs")] + [("top_n", C.c_int32), ("_pad", C.c_int32)]
+
+
+class hf_logprobs_grad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("norm", "entropy", "grad_logprob", "grad_entropy", "dlogits")] + [("dlogits_stride", C.c_int64)]
 
 
 hf_plan_p = C.c_void_p
@@ -131,6 +169,11 @@ SIGNATURES = {
     "hf_plan_check_buffers": (C.c_int, [_P, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t]),
     "hf_debug_restrict_kinds": (C.c_int, [_P, C.c_int]),
     "hf_plan_validate": (C.c_int, [_P]),
+    "hf_append_kv": (C.c_int, [C.POINTER(hf_kv_cache), C.POINTER(hf_append), C.c_void_p]),
+    "hf_attend_workspace_bytes": (C.c_size_t, [C.POINTER(hf_kv_cache), C.POINTER(hf_attention)]),
+    "hf_attend": (C.c_int, [C.POINTER(hf_kv_cache), C.POINTER(hf_attention), C.c_void_p]),
+    "hf_token_logprobs": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_logprobs), C.c_void_p]),
+    "hf_token_logprobs_back": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_logprobs_grad), C.c_void_p]),
     "hf_last_error": (C.c_char_p, []),
     "hf_version": (C.c_char_p, []),
 }

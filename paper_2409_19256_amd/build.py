@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhfreshard.so")
 BENCH_EXE = os.path.join(PKG, "hfbench")
-SOURCES = ["planner.cpp", "reshard_kernels.hip", "abi.hip"]
+SOURCES = ["planner.cpp", "reshard_kernels.hip", "abi.hip", "append_kernels.hip", "attend_kernels.hip", "logprob_kernels.hip", "rollout_abi.hip"]
 
 
 def hipcc() -> str:

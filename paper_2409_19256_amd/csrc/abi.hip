@@ -326,6 +326,15 @@ int launch_auto(const hf::Plan &p, const void *src, void *dst, void *stream) {
 
 } // namespace
 
+int hf::set_error(int code, const char *text) noexcept {
+  try {
+    g_err = text;
+  } catch (const std::bad_alloc &) {
+    g_err.clear();
+  }
+  return code;
+}
+
 extern "C" {
 
 int hf_reshard_plan(const hf_model_desc *model, const hf_train_layout *train, const hf_gen_layout *gen, hf_plan **out) {

@@ -7,6 +7,8 @@
 #include "slots.hpp"
 
 namespace hf {
+// Sets the calling thread's hf_last_error() and returns `code`; a text that finds no memory is left out.  (abi.hip)
+int set_error(int code, const char *text) noexcept;
 // Further variants of launch_tiles: reshard_auto over Plan::dev_auto.  extra_dst holds its distances, cache_policy is 1 or
 // 5, grid_wgs the number of workgroups that a CU may hold at a time (0 = as many as there is room for).  Paced: a wavefront's
 // stores wait for one another; workgroups of 64 lanes.  Otherwise of 64 (cache_policy 1) or kAutoShortThreads.  16 bytes a lane (part_bytes).
