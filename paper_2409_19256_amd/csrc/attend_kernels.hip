@@ -24,6 +24,7 @@
 
 #include <algorithm>
 
+#include "lanes.hpp"
 #include "rollout_kernels.hpp"
 
 namespace hf {
@@ -78,27 +79,6 @@ template <typename T> __device__ __forceinline__ uint32_t load_two(const char *r
   const uint16_t *e = reinterpret_cast<const uint16_t *>(row);
   const uint32_t lo = d < head_dim ? e[d] : 0, hi = d + 1 < head_dim ? e[d + 1] : 0;
   return lo | hi << 16;
-}
-
-// x of a lane and of the lane 32 (16) further, in either order: the instruction exchanges the upper half (odd rows of 16) of one register with the
-// lower half (even rows) of the other.  Written by hand because the compiler's builtin gives its first result for both; the two
-// wait states are those it puts between a write of the operands and the exchange.
-__device__ __forceinline__ void swap32(float &a, float &b) { asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b)); }
-__device__ __forceinline__ void swap16(float &a, float &b) { asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b)); }
-// the largest of the four lanes that share a column, and their sum
-__device__ __forceinline__ float column_max(float x) {
-  float y = x;
-  swap32(x, y);
-  x = y = fmaxf(x, y);
-  swap16(x, y);
-  return fmaxf(x, y);
-}
-__device__ __forceinline__ float column_sum(float x) {
-  float y = x;
-  swap32(x, y);
-  x = y = x + y;
-  swap16(x, y);
-  return x + y;
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack(float a, float b) {
@@ -299,7 +279,7 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-        const float m_new = fmaxf(m[n], column_max(top));
+        const float m_new = fmaxf(m[n], over_rows<Max>(top));
         if (__builtin_amdgcn_ballot_w64(m_new > m[n]) != 0) {
           const float keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[n] - m_new) * scale2);
           m[n] = m_new;
@@ -370,7 +350,7 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
   };
 
 #pragma unroll
-  for (int n = 0; n < kQ; ++n) l[n] = column_sum(l[n]);
+  for (int n = 0; n < kQ; ++n) l[n] = over_rows<Sum>(l[n]);
   if constexpr (kTokenWaves == 1) {
 #pragma unroll
     for (int n = 0; n < kQ; ++n) {
