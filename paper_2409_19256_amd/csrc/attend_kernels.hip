@@ -11,7 +11,9 @@
 // HBM is the bound there; a prompt's for all of its samples' rows.  What keeps the loads wide and the wavefronts fed:
 //  - a wavefront takes tiles of 32 tokens straight from memory into registers, keys and values of the next tile on their way while it works on
 //    the present one; nothing is staged and no wavefront waits for another until its part is done.  Where a prompt has many
-//    rows the wavefronts of a workgroup take different rows over the same tokens and meet in the L1 cache;
+//    rows, eight wavefronts of a workgroup share its tokens and rows, so that a SIMD has two (prompts brought into LDS by the whole workgroup were
+//    no faster: 54 us where this takes 52, 61 samples of 32749 tokens with 488 rows; it is bound by the vector unit, 41 % of its issue slots);
+//  - what is read for one workgroup alone goes past the caches (responses of the 7B shape, 1024 tokens each: 6.8 TB/s, plain loads 6.0);
 //  - a page's number and address are the same for a whole wavefront and are worked out by the scalar unit (pages of 16 tokens and more);
 //  - scores are made transposed, S^T = K Q^T: the accumulator then holds, for the query of a lane's column, four tokens of each 16, which
 //    is what the second product O^T = V^T P^T wants as its right operand if its 32 tokens are taken in the order (16-token
@@ -31,7 +33,7 @@ namespace hf {
 
 namespace {
 
-constexpr int kThreads = 256, kWave = 64, kWaves = kThreads / kWave;
+constexpr int kThreads = 256, kWave = 64;
 constexpr int kTile = 32;   // tokens of a tile
 constexpr int kRowsTile = 16; // queries of a tile
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -99,41 +101,37 @@ __device__ __forceinline__ Members members(const hf_attention &a, int g) {
   return {first, min(last - first, a.max_group)};
 }
 
-// Rows row0 .. of a segment (the sequences [first, first + n), all of which see its tokens) over its tokens [begin, end).  kRowWaves wavefronts
-// have kQ * 16 rows each, and the others the same rows over other tokens.
-template <typename T, int kDim, int kQ, int kRowWaves, int kMode, bool kLanes>
-__device__ __forceinline__ void part(const AttendParams &p, const int32_t *table, int begin, int end, Members who, int row0, int kv_head, int part_index,
-                                     float *shared) {
-  constexpr int kSteps = kDim / 32; // of the first product
-  constexpr int kOwn = kDim / 16;   // elements of a value row that a lane holds, products of the second kind
-  constexpr int kTokenWaves = kWaves / kRowWaves;
-  const hf_attention &a = p.a;
-  const int lane = threadIdx.x % kWave, col = lane % 16, grp = lane / 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
-  const int rows = who.n * p.ratio, my_row0 = row0 + row_wave * kQ * kRowsTile;
-  const char *keys = p.k + kv_head * p.head_bytes, *values = p.v + kv_head * p.head_bytes;
-  const int in_page = (1 << p.page_shift) - 1;
+// How a wavefront finds and reads tiles, and what it does with them.
+template <typename T, int kDim, int kMode, bool kLanes, bool kOnce> struct Reader {
+  static constexpr int kSteps = kDim / 32; // of the first product
+  static constexpr int kOwn = kDim / 16;   // elements of a value row that a lane holds, products of the second kind
+  const AttendParams &p;
+  const int col = threadIdx.x % 16, grp = threadIdx.x % kWave / 16, in_page = (1 << p.page_shift) - 1;
+  // pieces past the head are read from its start, and left out when the result is written
+  const uint32_t value_piece = kMode == kPieces && kOwn * col >= p.head_dim ? 0 : 2 * kOwn * col;
+  const uint32_t k_lane = kLanes ? 0 : col * (uint32_t)p.token_bytes + 16 * grp;
+  const uint32_t v_lane[4] = {first_value(0), first_value(1), first_value(2), first_value(3)};
+  const float scale2 = fabsf(p.scale2);
 
-  u32x4 q[kQ][kSteps];
-#pragma unroll
-  for (int n = 0; n < kQ; ++n) {
-    const int row = my_row0 + n * kRowsTile + col;
-    const int seq = who.first + row / p.ratio, head = kv_head * p.ratio + row % p.ratio;
-    const char *from = static_cast<const char *>(a.q) + (seq * a.q_stride + head * a.q_head_stride) * (int64_t)sizeof(T);
+  __device__ __forceinline__ uint32_t first_value(int i) const { return kLanes ? 0 : (4 * grp + i) * (uint32_t)p.token_bytes + value_piece; }
+
+  // the queries of row (counted over the sequences from `first` on) of the rows that read one KV head
+  __device__ __forceinline__ void load_queries(u32x4 (&q)[kSteps], int first, int row, int rows, int kv_head) const {
+    const int seq = first + row / p.ratio, head = kv_head * p.ratio + row % p.ratio;
+    const char *from = static_cast<const char *>(p.a.q) + (seq * p.a.q_stride + head * p.a.q_head_stride) * (int64_t)sizeof(T);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int d = 32 * s + 8 * grp;
-      q[n][s] = u32x4{};
+      q[s] = u32x4{};
       if constexpr (kMode == kElements) {
         if (row < rows)
-          for (int e = 0; e < 4; ++e) q[n][s][e] = load_two<T>(from, d + 2 * e, p.head_dim);
+          for (int e = 0; e < 4; ++e) q[s][e] = load_two<T>(from, d + 2 * e, p.head_dim);
       } else if (row < rows && (kMode == kWhole || d < p.head_dim)) {
-        q[n][s] = *reinterpret_cast<const u32x4 *>(from + 2 * d);
+        q[s] = *reinterpret_cast<const u32x4 *>(from + 2 * d);
       }
-      if (p.scale2 < 0) q[n][s] ^= 0x80008000u; // the maximum is taken of the products, so the scale has to be positive
+      if (p.scale2 < 0) q[s] ^= 0x80008000u; // the maximum is taken of the products, so the scale has to be positive
     }
   }
-  const float scale2 = fabsf(p.scale2);
 
   // Where a tile's tokens are.  A page of 16 tokens or more holds a half of a tile whole, so that its number is the same for all lanes and is
   // fetched and turned into an address by the scalar unit; with smaller pages every lane has its own.
@@ -141,10 +139,10 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
     int k[2], v[2];
   };
   struct At {
-    int64_t k[2], v[2]; // bytes from the head's first element
+    int64_t k[2], v[2]; // bytes from the cache's first element
     bool ok[2];
   };
-  const auto pages_at = [&](int token) {
+  __device__ __forceinline__ Pages pages_at(const int32_t *table, int token, int end) const {
     Pages g;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -156,34 +154,34 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
       }
     }
     return g;
-  };
+  }
   // an unusable page number stands for page 0, whose tokens are then not seen
-  const auto page_bytes = [&](int page) { return (int64_t)((uint32_t)page < p.n_pages ? (uint32_t)page : 0u) * p.page_bytes; };
-  const auto place = [&](const Pages &g, int token) {
+  __device__ __forceinline__ int64_t page_bytes(int page) const { return (int64_t)((uint32_t)page < p.n_pages ? (uint32_t)page : 0u) * p.page_bytes; }
+  __device__ __forceinline__ At place(const Pages &g, int token, int kv_head) const {
+    const int64_t head = kv_head * p.head_bytes;
     At at;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       at.ok[h] = (uint32_t)g.v[h] < p.n_pages;
       if constexpr (kLanes) {
-        at.k[h] = page_bytes(g.k[h]) + ((token + 16 * h + col) & in_page) * p.token_bytes + 16 * grp;
-        at.v[h] = page_bytes(g.v[h]) + ((token + 16 * h + 4 * grp) & in_page) * p.token_bytes + 2 * kOwn * col;
+        at.k[h] = head + page_bytes(g.k[h]) + ((token + 16 * h + col) & in_page) * p.token_bytes + 16 * grp;
+        at.v[h] = head + page_bytes(g.v[h]) + ((token + 16 * h + 4 * grp) & in_page) * p.token_bytes + 2 * kOwn * col;
       } else {
-        at.k[h] = at.v[h] = page_bytes(g.k[h]) + ((token + 16 * h) & in_page) * p.token_bytes;
+        at.k[h] = at.v[h] = head + page_bytes(g.k[h]) + ((token + 16 * h) & in_page) * p.token_bytes;
       }
     }
     return at;
-  };
-  // pieces past the head are read from its start, and left out when the result is written
-  const uint32_t value_piece = kMode == kPieces && kOwn * col >= p.head_dim ? 0 : 2 * kOwn * col;
-  const uint32_t k_lane = kLanes ? 0 : col * (uint32_t)p.token_bytes + 16 * grp;
-  uint32_t v_lane[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v_lane[i] = kLanes ? 0 : (4 * grp + i) * (uint32_t)p.token_bytes + value_piece;
+  }
 
-  const auto load_keys = [&](u32x4(&k)[2][kSteps], const At &at) {
+  // what one wavefront alone reads goes past the caches
+  static __device__ __forceinline__ u32x4 load16(const char *from) {
+    const u32x4 *at = reinterpret_cast<const u32x4 *>(from);
+    return kOnce ? __builtin_nontemporal_load(at) : *at;
+  }
+  __device__ __forceinline__ void load_keys(u32x4 (&k)[2][kSteps], const At &at) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char *row = keys + at.k[h];
+      const char *row = p.k + at.k[h];
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const int d = 32 * s + 8 * grp;
@@ -191,30 +189,30 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
           for (int e = 0; e < 4; ++e) k[h][s][e] = load_two<T>(row - 16 * grp, d + 2 * e, p.head_dim);
         } else if constexpr (kMode == kPieces) {
           k[h][s] = u32x4{};
-          if (d < p.head_dim) k[h][s] = *reinterpret_cast<const u32x4 *>(row + k_lane + 64 * s);
+          if (d < p.head_dim) k[h][s] = load16(row + k_lane + 64 * s);
         } else {
-          k[h][s] = *reinterpret_cast<const u32x4 *>(row + k_lane + 64 * s);
+          k[h][s] = load16(row + k_lane + 64 * s);
         }
       }
     }
-  };
-  const auto load_values = [&](uint32_t(&v)[8][kOwn / 2], const At &at) {
+  }
+  __device__ __forceinline__ void load_values(uint32_t (&v)[8][kOwn / 2], const At &at) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const char *row = kLanes ? values + at.v[h] + i * p.token_bytes : values + at.v[h] + v_lane[i];
+        const char *row = kLanes ? p.v + at.v[h] + i * p.token_bytes : p.v + at.v[h] + v_lane[i];
         if constexpr (kMode == kElements) {
           for (int e = 0; e < kOwn / 2; ++e) v[4 * h + i][e] = load_two<T>(row - 2 * kOwn * col, kOwn * col + 2 * e, p.head_dim);
         } else {
           if constexpr (kLanes) row += (int)value_piece - 2 * kOwn * col;
           if constexpr (kOwn == 4) {
-            const u32x2 x = *reinterpret_cast<const u32x2 *>(row);
+            const u32x2 x = kOnce ? __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(row)) : *reinterpret_cast<const u32x2 *>(row);
             v[4 * h + i][0] = x[0], v[4 * h + i][1] = x[1];
           } else {
 #pragma unroll
             for (int e = 0; e < kOwn / 8; ++e) { // the second piece of 16 elements may be past the head too
-              const u32x4 x = *reinterpret_cast<const u32x4 *>(row + (kMode == kPieces && e && kOwn * col + 8 >= p.head_dim ? 0 : 16 * e));
+              const u32x4 x = load16(row + (kMode == kPieces && e && kOwn * col + 8 >= p.head_dim ? 0 : 16 * e));
 #pragma unroll
               for (int f = 0; f < 4; ++f) v[4 * h + i][4 * e + f] = x[f];
             }
@@ -222,15 +220,182 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
         }
       }
     }
+  }
+
+  // which of the lane's tokens are visible; true if all of the tile's are
+  __device__ __forceinline__ bool visible(bool (&seen)[8], const At &at, int token, int end) const {
+    const bool whole = token + kTile <= end && (kLanes ? __builtin_amdgcn_ballot_w64(!(at.ok[0] && at.ok[1])) == 0 : at.ok[0] && at.ok[1]);
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) seen[i] = at.ok[i / 4] && token + 16 * (i / 4) + 4 * grp + i % 4 < end;
+    }
+    return whole;
+  }
+  static __device__ __forceinline__ void scores(f32x4 (&s)[2], const u32x4 (&k)[2][kSteps], const u32x4 (&q)[kSteps]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s[h] = f32x4{};
+#pragma unroll
+      for (int e = 0; e < kSteps; ++e) s[h] = Matrix<T>::product(k[h][e], q[e], s[h]);
+    }
+  }
+  // what is not visible may hold anything, and 0 * NaN is no 0
+  static __device__ __forceinline__ void blank(uint32_t (&v)[8][kOwn / 2], const bool (&seen)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < kOwn / 2; ++e) v[i][e] = seen[i] ? v[i][e] : 0;
+  }
+  // eight tokens of element kOwn * col + j, as a left operand
+  static __device__ __forceinline__ u32x4 turned(const uint32_t (&v)[8][kOwn / 2], int j) {
+    u32x4 left;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) left[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+    return left;
+  }
+};
+
+// 16 rows' softmax so far; m of the products, before the scale.  m follows the largest score only when one is past it by kSlack of base 2 (P is
+// then below 2^kSlack): with 16 rows to a tile some row has a new largest score in nearly every tile, and everything would be rescaled each time.
+constexpr float kSlack = 8;
+template <typename T, int kOwn> struct Rows {
+  f32x4 o[kOwn];
+  float m, l, limit; // limit: m and the slack
+  __device__ __forceinline__ void clear() {
+    m = limit = -INFINITY, l = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) o[j] = f32x4{};
+  }
+  // a tile's scores join the maximum and the sum, and become P in two halves
+  __device__ __forceinline__ void join(const f32x4 (&s)[2], bool whole, const bool (&seen)[8], float scale2, u32x4 &hi, u32x4 &lo) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4];
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = seen[i] ? x[i] : -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+    if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
+      const float m_new = fmaxf(m, over_rows<Max>(top));
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
+      m = m_new;
+      limit = m + kSlack / scale2;
+      l *= keep;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) o[j] *= keep;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * scale2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale2, base));
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = seen[i] ? x[i] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) l += x[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      hi[i] = pack<T>(x[2 * i], x[2 * i + 1]);
+      lo[i] = pack<T>(x[2 * i] - unpack<T>(hi[i], 0), x[2 * i + 1] - unpack<T>(hi[i], 1));
+    }
+  }
+  __device__ __forceinline__ void add(int j, u32x4 left, u32x4 hi, u32x4 lo) { o[j] = Matrix<T>::product(left, lo, Matrix<T>::product(left, hi, o[j])); }
+};
+
+// a row's output and lse from its sums; acc: kN elements from d0 on
+template <typename T, int kN, int kMode>
+__device__ __forceinline__ void write_row(const AttendParams &p, int seq, int head, int d0, float m2, float sum, const float *acc) {
+  const hf_attention &a = p.a;
+  const float scale = sum == 0 ? 0.f : 1 / sum;
+  T *to = static_cast<T *>(a.out) + seq * a.out_stride + head * a.out_head_stride + d0;
+#pragma unroll
+  for (int e = 0; e < kN; ++e)
+    if (kMode == kWhole || d0 + e < p.head_dim) to[e] = (T)(acc[e] * scale);
+  if (a.lse && d0 == 0) a.lse[(int64_t)seq * a.n_q_heads + head] = sum == 0 ? -INFINITY : (m2 + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+// a row's partial result
+template <int kN, int kMode> __device__ __forceinline__ void write_part(const AttendParams &p, int64_t slot, int d0, float top, float m2, float sum, const float *acc) {
+  float *to = p.part_o + slot * p.head_dim + d0;
+  if constexpr (kMode == kWhole) {
+#pragma unroll
+    for (int e = 0; e < kN; e += 4) *reinterpret_cast<f32x4 *>(to + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < kN; ++e)
+      if (d0 + e < p.head_dim) to[e] = acc[e];
+  }
+  if (d0 == 0) p.part_ml[2 * slot] = top == -INFINITY ? -INFINITY : m2, p.part_ml[2 * slot + 1] = sum;
+}
+
+// The parts of a workgroup's wavefronts become one: kRowWaves of them have rows of their own, the others the same rows over other tokens.
+template <typename T, int kDim, int kWaves, int kQ, int kRowWaves, int kMode>
+__device__ __forceinline__ void join_waves(const AttendParams &p, Rows<T, kDim / 16> (&r)[kQ], Members who, int row0, int kv_head, int part_index, float scale2, float *shared) {
+  constexpr int kOwn = kDim / 16, kTokenWaves = kWaves / kRowWaves;
+  const int rows = who.n * p.ratio, col = threadIdx.x % 16, grp = threadIdx.x % kWave / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
+  const auto write = [&](int row, int d0, float top, float sum, const float *acc) {
+    const int seq = who.first + row / p.ratio, head = kv_head * p.ratio + row % p.ratio;
+    if (p.s.direct) write_row<T, kOwn, kMode>(p, seq, head, d0, top * scale2, sum, acc);
+    else write_part<kOwn, kMode>(p, ((int64_t)seq * p.a.n_q_heads + head) * (p.s.prefix_parts + p.s.suffix_parts) + part_index, d0, top, top * scale2, sum, acc);
   };
 
-  f32x4 o[kQ][kOwn];
-  float m[kQ], l[kQ]; // m of the products, before the scale
+#pragma unroll
+  for (int n = 0; n < kQ; ++n) r[n].l = over_rows<Sum>(r[n].l);
+  constexpr int kPitch = kDim + 4, kRows = kRowWaves * kRowsTile;
+  float *const both = shared + kTokenWaves * kRows * kPitch; // [token wave, row, 2]
 #pragma unroll
   for (int n = 0; n < kQ; ++n) {
-    m[n] = -INFINITY, l[n] = 0;
+    if (n) __syncthreads();
+    const int mine = token_wave * kRows + row_wave * kRowsTile + col;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) o[n][j] = f32x4{};
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) shared[mine * kPitch + kOwn * (4 * grp + i) + j] = r[n].o[j][i];
+    if (grp == 0) both[2 * mine] = r[n].m, both[2 * mine + 1] = r[n].l;
+    __syncthreads();
+#pragma unroll
+    for (int r0 = 0; r0 < kRows; r0 += kWaves * kWave / 16) {
+      const int at = r0 + threadIdx.x / 16, d0 = threadIdx.x % 16 * kOwn;
+      const int row = row0 + (at / kRowsTile * kQ + n) * kRowsTile + at % kRowsTile;
+      if (at < kRows && row < rows) {
+        float top = -INFINITY, sum = 0, acc[kOwn] = {};
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w) top = fmaxf(top, both[2 * (w * kRows + at)]);
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w) {
+          const float mw = both[2 * (w * kRows + at)], weight = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - top) * scale2);
+          sum += weight * both[2 * (w * kRows + at) + 1];
+#pragma unroll
+          for (int e = 0; e < kOwn; ++e) acc[e] += weight * shared[(w * kRows + at) * kPitch + d0 + e];
+        }
+        write(row, d0, top, sum, acc);
+      }
+    }
+  }
+}
+
+// Rows row0 .. of a segment (the sequences [first, first + n), all of which see its tokens) over its tokens [begin, end).  kRowWaves wavefronts
+// have kQ * 16 rows each, and the others the same rows over other tokens.
+template <typename T, int kDim, int kWaves, int kQ, int kRowWaves, int kMode, bool kLanes, bool kOnce>
+__device__ __forceinline__ void part(const AttendParams &p, const int32_t *table, int begin, int end, Members who, int row0, int kv_head, int part_index,
+                                     float *shared) {
+  typedef Reader<T, kDim, kMode, kLanes, kOnce> R;
+  constexpr int kSteps = R::kSteps, kOwn = R::kOwn, kTokenWaves = kWaves / kRowWaves;
+  const R reader = {p};
+  const int col = reader.col;
+  const float scale2 = reader.scale2;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
+  const int rows = who.n * p.ratio, my_row0 = row0 + row_wave * kQ * kRowsTile;
+
+  u32x4 q[kQ][kSteps];
+  Rows<T, kOwn> r[kQ];
+#pragma unroll
+  for (int n = 0; n < kQ; ++n) {
+    reader.load_queries(q[n], who.first, my_row0 + n * kRowsTile + col, rows, kv_head);
+    r[n].clear();
   }
 
   // Page numbers are fetched two tiles ahead.  The next tile's keys are on their way from when the scores are made, its values from when they are added
@@ -240,195 +405,90 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
   if (token < end && my_row0 < rows) {
     u32x4 k[2][kSteps];
     uint32_t v[8][kOwn / 2];
-    At at = place(pages_at(token), token);
-    Pages next = pages_at(token + kStep);
-    load_keys(k, at);
-    load_values(v, at);
+    typename R::At at = reader.place(reader.pages_at(table, token, end), token, kv_head);
+    typename R::Pages next = reader.pages_at(table, token + kStep, end);
+    reader.load_keys(k, at);
+    reader.load_values(v, at);
     for (;;) {
       const bool more = token + kStep < end;
-      const bool whole = token + kTile <= end && (kLanes ? __builtin_amdgcn_ballot_w64(!(at.ok[0] && at.ok[1])) == 0 : at.ok[0] && at.ok[1]);
       bool seen[8];
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) seen[i] = at.ok[i / 4] && token + 16 * (i / 4) + 4 * grp + i % 4 < end;
-      }
+      const bool whole = reader.visible(seen, at, token, end);
       f32x4 s[kQ][2];
 #pragma unroll
-      for (int n = 0; n < kQ; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          s[n][h] = f32x4{};
-#pragma unroll
-          for (int e = 0; e < kSteps; ++e) s[n][h] = Matrix<T>::product(k[h][e], q[n][e], s[n][h]);
-        }
-      at = place(next, token + kStep);
+      for (int n = 0; n < kQ; ++n) R::scores(s[n], k, q[n]);
+      at = reader.place(next, token + kStep, kv_head);
       if (more) {
-        next = pages_at(token + 2 * kStep);
-        load_keys(k, at);
+        next = reader.pages_at(table, token + 2 * kStep, end);
+        reader.load_keys(k, at);
       }
       u32x4 hi[kQ], lo[kQ];
 #pragma unroll
-      for (int n = 0; n < kQ; ++n) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[n][i / 4][i % 4];
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = seen[i] ? x[i] : -INFINITY;
-        }
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-        const float m_new = fmaxf(m[n], over_rows<Max>(top));
-        if (__builtin_amdgcn_ballot_w64(m_new > m[n]) != 0) {
-          const float keep = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[n] - m_new) * scale2);
-          m[n] = m_new;
-          l[n] *= keep;
-#pragma unroll
-          for (int j = 0; j < kOwn; ++j) o[n][j] *= keep;
-        }
-        const float base = m[n] == -INFINITY ? 0.f : -m[n] * scale2;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale2, base));
-        if (!whole) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = seen[i] ? x[i] : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l[n] += x[i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          hi[n][i] = pack<T>(x[2 * i], x[2 * i + 1]);
-          lo[n][i] = pack<T>(x[2 * i] - unpack<T>(hi[n][i], 0), x[2 * i + 1] - unpack<T>(hi[n][i], 1));
-        }
-      }
-      if (!whole) { // what is not visible may hold anything, and 0 * NaN is no 0
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int e = 0; e < kOwn / 2; ++e) v[i][e] = seen[i] ? v[i][e] : 0;
-      }
+      for (int n = 0; n < kQ; ++n) r[n].join(s[n], whole, seen, scale2, hi[n], lo[n]);
+      if (!whole) R::blank(v, seen);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) {
-        u32x4 left;
+        const u32x4 left = R::turned(v, j);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) left[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-        for (int n = 0; n < kQ; ++n) o[n][j] = Matrix<T>::product(left, lo[n], Matrix<T>::product(left, hi[n], o[n][j]));
+        for (int n = 0; n < kQ; ++n) r[n].add(j, left, hi[n], lo[n]);
       }
       token += kStep;
       if (!more) break;
-      load_values(v, at);
+      reader.load_values(v, at);
     }
   }
 
-  // a row's sum and output, or its part of them
-  const auto write = [&](int row, int d0, float top, float sum, const float *acc) {
-    const int seq = who.first + row / p.ratio, head = kv_head * p.ratio + row % p.ratio;
-    const int64_t at = (int64_t)seq * a.n_q_heads + head;
-    const float m2 = top * scale2;
-    if (p.s.direct) {
-      const float scale = sum == 0 ? 0.f : 1 / sum;
-      T *to = static_cast<T *>(a.out) + seq * a.out_stride + head * a.out_head_stride + d0;
-#pragma unroll
-      for (int e = 0; e < kOwn; ++e)
-        if (kMode == kWhole || d0 + e < p.head_dim) to[e] = (T)(acc[e] * scale);
-      if (a.lse && d0 == 0) a.lse[at] = sum == 0 ? -INFINITY : (m2 + __builtin_amdgcn_logf(sum)) * kLn2;
-    } else {
-      const int64_t slot = at * (p.s.prefix_parts + p.s.suffix_parts) + part_index;
-      float *to = p.part_o + slot * p.head_dim + d0;
-      if constexpr (kMode == kWhole) {
-#pragma unroll
-        for (int e = 0; e < kOwn; e += 4) *reinterpret_cast<f32x4 *>(to + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-      } else {
-#pragma unroll
-        for (int e = 0; e < kOwn; ++e)
-          if (d0 + e < p.head_dim) to[e] = acc[e];
-      }
-      if (d0 == 0) p.part_ml[2 * slot] = top == -INFINITY ? -INFINITY : m2, p.part_ml[2 * slot + 1] = sum;
-    }
-  };
-
-#pragma unroll
-  for (int n = 0; n < kQ; ++n) l[n] = over_rows<Sum>(l[n]);
-  if constexpr (kTokenWaves == 1) {
-#pragma unroll
-    for (int n = 0; n < kQ; ++n) {
-      const int row = my_row0 + n * kRowsTile + col;
-      if (row < rows) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float acc[kOwn];
-#pragma unroll
-          for (int j = 0; j < kOwn; ++j) acc[j] = o[n][j][i];
-          write(row, kOwn * (4 * grp + i), m[n], l[n], acc);
-        }
-      }
-    }
-  } else { // the wavefronts' parts become one
-    constexpr int kPitch = kDim + 4, kRows = kRowWaves * kRowsTile;
-    float *const both = shared + kTokenWaves * kRows * kPitch; // [token wave, row, 2]
-#pragma unroll
-    for (int n = 0; n < kQ; ++n) {
-      if (n) __syncthreads();
-      const int mine = token_wave * kRows + row_wave * kRowsTile + col;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < kOwn; ++j) shared[mine * kPitch + kOwn * (4 * grp + i) + j] = o[n][j][i];
-      if (grp == 0) both[2 * mine] = m[n], both[2 * mine + 1] = l[n];
-      __syncthreads();
-#pragma unroll
-      for (int r0 = 0; r0 < kRows; r0 += kThreads / 16) {
-        const int r = r0 + threadIdx.x / 16, d0 = threadIdx.x % 16 * kOwn;
-        const int row = row0 + (r / kRowsTile * kQ + n) * kRowsTile + r % kRowsTile;
-        if (row < rows) {
-          float top = -INFINITY, sum = 0, acc[kOwn] = {};
-#pragma unroll
-          for (int w = 0; w < kTokenWaves; ++w) top = fmaxf(top, both[2 * (w * kRows + r)]);
-#pragma unroll
-          for (int w = 0; w < kTokenWaves; ++w) {
-            const float mw = both[2 * (w * kRows + r)], weight = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - top) * scale2);
-            sum += weight * both[2 * (w * kRows + r) + 1];
-#pragma unroll
-            for (int e = 0; e < kOwn; ++e) acc[e] += weight * shared[(w * kRows + r) * kPitch + d0 + e];
-          }
-          write(row, d0, top, sum, acc);
-        }
-      }
-    }
-  }
+  join_waves<T, kDim, kWaves, kQ, kRowWaves, kMode>(p, r, who, row0, kv_head, part_index, scale2, shared);
 }
 
-template <typename T, int kDim, int kQ, int kRowWaves, int kMode, bool kLanes>
-__global__ __launch_bounds__(kThreads, kDim > 128 || kMode == kElements ? 1 : 2) void attend_parts(AttendParams p) {
+// The sequence with the n-th longest response (equal ones in order), of at most kThreads.  Workgroups are handed out in order: with the longest first
+// the last ones to run are short.
+template <int kThreads> __device__ __forceinline__ int nth_longest(const AttendParams &p, int n) {
+  __shared__ __attribute__((aligned(16))) int lens[kThreads];
+  __shared__ int found;
+  const int t = threadIdx.x, own = t < p.a.n_seqs ? max(min(p.a.suffix_lens[t], p.s.max_suffix), 0) : -1;
+  lens[t] = own;
+  __syncthreads();
+  int rank = 0;
+  for (int j = 0; j < p.a.n_seqs; j += 4) {
+    const int4 x = *reinterpret_cast<const int4 *>(lens + j);
+    rank += (x.x > own || (x.x == own && j < t)) + (x.y > own || (x.y == own && j + 1 < t)) + (x.z > own || (x.z == own && j + 2 < t)) +
+            (x.w > own || (x.w == own && j + 3 < t));
+  }
+  if (t < p.a.n_seqs && rank == n) found = t;
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(found);
+}
+
+// The parts of prompts and of responses; both in one grid where prompts have few rows too.
+template <typename T, int kDim, int kWaves, int kQ, int kRowWaves, int kMode, bool kLanes, bool kOnce>
+__global__ __launch_bounds__(kWaves * kWave, kDim > 128 || kMode == kElements ? 1 : kQ > 1 || kDim > 64 ? 2 : 3) void attend_parts(AttendParams p, uint32_t prefix_wgs) {
   __shared__ float shared[kWaves * kRowsTile * (kDim + 4 + 2)];
   const hf_attention &a = p.a;
   uint32_t id = blockIdx.x;
-  if (id < p.s.prefix_wgs) {
+  if (id < prefix_wgs) {
     // the query blocks of a part follow one another on one XCD (workgroups go round over the eight), where L2 holds the part's keys and values for them
     const uint32_t xcd = id % 8, turn = id / 8, block = turn % p.s.prefix_blocks;
     uint32_t item = turn / p.s.prefix_blocks * 8 + xcd;
     const int kv_head = item % p.n_kv_heads;
     item /= p.n_kv_heads;
-    const int index = item % p.s.prefix_parts, g = item / p.s.prefix_parts;
-    if (g >= a.n_groups) return;
+    const int g = item % a.n_groups, index = item / a.n_groups;
+    if (index >= p.s.prefix_parts) return;
     const int begin = index * p.s.prefix_chunk, end = min(min(a.prefix_lens[g], p.s.max_prefix), begin + p.s.prefix_chunk);
     const Members who = members(a, g);
     const int row0 = block * kRowWaves * kQ * kRowsTile;
     if (begin >= end || row0 >= who.n * p.ratio) return;
-    part<T, kDim, kQ, kRowWaves, kMode, kLanes>(p, a.prefix_pages + (int64_t)g * a.prefix_width, begin, end, who, row0, kv_head, index, shared);
-  } else {
-    id -= p.s.prefix_wgs;
+    part<T, kDim, kWaves, kQ, kRowWaves, kMode, kLanes, kOnce>(p, a.prefix_pages + (int64_t)g * a.prefix_width, begin, end, who, row0, kv_head, index, shared);
+  } else if constexpr (kQ * kRowWaves == 1) {
+    id -= prefix_wgs;
     const int kv_head = id % p.n_kv_heads;
     id /= p.n_kv_heads;
     const int block = id % p.s.suffix_blocks;
     id /= p.s.suffix_blocks;
-    const int index = id % p.s.suffix_parts, seq = id / p.s.suffix_parts;
+    const int seq = p.s.ordered ? nth_longest<kWaves * kWave>(p, id % a.n_seqs) : id % a.n_seqs, index = id / a.n_seqs;
     const int begin = index * p.s.suffix_chunk, end = min(min(a.suffix_lens[seq], p.s.max_suffix), begin + p.s.suffix_chunk);
     if (begin >= end && !p.s.direct) return;
-    part<T, kDim, 1, 1, kMode, kLanes>(p, a.suffix_pages + (int64_t)seq * a.suffix_width, begin, end, Members{seq, 1}, block * kRowsTile, kv_head,
-                                       p.s.prefix_parts + index, shared);
+    part<T, kDim, kWaves, 1, 1, kMode, kLanes, kOnce>(p, a.suffix_pages + (int64_t)seq * a.suffix_width, begin, end, Members{seq, 1}, block * kRowsTile, kv_head,
+                                                      p.s.prefix_parts + index, shared);
   }
 }
 
@@ -506,28 +566,33 @@ template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void atte
   if (a.lse && lane == 0) a.lse[row] = sum == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <typename T, int kDim, int kQ, int kRowWaves, int kMode, bool kLanes> hipError_t launch_shape(const AttendParams &p, hipStream_t st) {
-  const hipError_t e = enqueue_kernel(attend_parts<T, kDim, kQ, kRowWaves, kMode, kLanes>, dim3((uint32_t)(p.s.prefix_wgs + p.s.suffix_wgs)), kThreads, st, p);
-  if (e != hipSuccess || p.s.direct) return e;
+template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, hipStream_t st) {
+  const AttendShape &s = p.s;
+  uint32_t prefix_wgs = (uint32_t)s.prefix_wgs;
+  hipError_t e = hipSuccess;
+  if constexpr (kDim <= 128 && kMode != kElements) {
+    if (s.row_waves) {
+      const dim3 grid(prefix_wgs);
+      e = s.row_waves == 4   ? enqueue_kernel(attend_parts<T, kDim, 8, 2, 4, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs)
+          : s.row_waves == 2 ? enqueue_kernel(attend_parts<T, kDim, 8, 2, 2, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs)
+                             : enqueue_kernel(attend_parts<T, kDim, 8, 2, 1, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs);
+      prefix_wgs = 0;
+    }
+  }
+  if (e == hipSuccess)
+    e = enqueue_kernel(attend_parts<T, kDim, 4, 1, 1, kMode, kLanes, true>, dim3((uint32_t)(prefix_wgs + s.suffix_wgs)), 4 * kWave, st, p, prefix_wgs);
+  if (e != hipSuccess || s.direct) return e;
   const int64_t rows = (int64_t)p.a.n_seqs * p.a.n_q_heads;
   constexpr int kTeams = kThreads / (kDim / 4);
   int split = 1;
-  while (split < kTeams && 4 * split < p.s.prefix_parts + p.s.suffix_parts) split *= 2;
+  while (split < kTeams && 4 * split < s.prefix_parts + s.suffix_parts) split *= 2;
   const int rows_of_wg = kTeams / split;
   return enqueue_kernel(attend_merge<T, kDim>, dim3((uint32_t)((rows + rows_of_wg - 1) / rows_of_wg)), kThreads, st, p, split);
 }
-template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_rows(const AttendParams &p, hipStream_t st) {
-  if constexpr (kDim <= 128 && kMode != kElements) {
-    if (p.s.row_waves == 4) return launch_shape<T, kDim, 2, 4, kMode, kLanes>(p, st);
-    if (p.s.row_waves == 2) return launch_shape<T, kDim, 2, 2, kMode, kLanes>(p, st);
-    if (p.s.q_tiles == 2) return launch_shape<T, kDim, 2, 1, kMode, kLanes>(p, st);
-  }
-  return launch_shape<T, kDim, 1, 1, kMode, kLanes>(p, st);
-}
 template <typename T, int kDim> hipError_t launch_dim(const AttendParams &p, bool vec, hipStream_t st) {
-  if (!vec) return launch_rows<T, kDim, kElements, true>(p, st);
-  if (p.head_dim != kDim) return launch_rows<T, kDim, kPieces, true>(p, st);
-  return p.s.lanes ? launch_rows<T, kDim, kWhole, true>(p, st) : launch_rows<T, kDim, kWhole, false>(p, st);
+  if (!vec) return launch_mode<T, kDim, kElements, true>(p, st);
+  if (p.head_dim != kDim) return launch_mode<T, kDim, kPieces, true>(p, st);
+  return p.s.lanes ? launch_mode<T, kDim, kWhole, true>(p, st) : launch_mode<T, kDim, kWhole, false>(p, st);
 }
 template <typename T> hipError_t launch_type(const AttendParams &p, bool vec, hipStream_t st) {
   if (p.head_dim <= 64) return launch_dim<T, 64>(p, vec, st);
@@ -542,28 +607,32 @@ AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool v
   const int64_t page = cache.page_tokens, ratio = a.n_q_heads / cache.n_kv_heads;
   s.max_suffix = (int32_t)std::min<int64_t>(a.max_suffix, std::min<int64_t>(a.suffix_width * page, 1 << 30));
   s.max_prefix = a.n_groups ? (int32_t)std::min<int64_t>(a.max_prefix, std::min<int64_t>(a.prefix_width * page, 1 << 30)) : 0;
-  // parts: as long as they may be while there are four workgroups a CU of responses, or one of prompts (whose parts cost every row a partial result:
-  // us at 256 / 512 / 1024 workgroups, 128 samples of 8 prompts with 128 rows to a KV head 146 / 173 / 195, 61 samples of one of 32749 tokens with 488 62 / 72 / 87)
+  // Parts are as long as they may be while there are `want` workgroups.  A workgroup starts up for some 5 us (length, page numbers, first tiles one after another) and
+  // every part costs its rows a partial result.  us at 1 / 2 / 4 / 8 parts a response, 128 responses of 2048 tokens (8 KV heads, eight rows each) 165 / 178 /
+  // 198 / 237, of 1 to 2048 tokens 94 / 104 / 114 / 140; prompts with 128 rows (8, of 2048) at 128 / 256 / 512 workgroups 48 / 32 / 40, with 488 (one, of 32749) 84 / 52 / 61.
   const auto chunk = [&](int64_t len, int64_t others, int64_t want) {
     int64_t c = 128;
     while (c < len && others * ((len + 2 * c - 1) / (2 * c)) >= want) c *= 2;
     return (int32_t)c;
   };
   const int64_t rows = std::min<int64_t>(a.max_group, a.n_seqs) * ratio;
-  s.q_tiles = vec && cache.head_dim <= 128 && rows > kRowsTile ? 2 : 1;
-  s.row_waves = s.q_tiles == 1 || rows <= 2 * kRowsTile ? 1 : rows <= 4 * kRowsTile ? 2 : 4;
+  const bool two = vec && cache.head_dim <= 128 && rows > kRowsTile;
+  s.row_waves = !two ? 0 : rows <= 2 * kRowsTile ? 1 : rows <= 4 * kRowsTile ? 2 : 4;
   s.lanes = page < 16 || cache.token_stride >= 1 << 25;
-  const int64_t rows_of_wg = s.q_tiles * s.row_waves * kRowsTile;
+  const int64_t rows_of_wg = two ? 2 * s.row_waves * kRowsTile : kRowsTile;
   s.prefix_blocks = (int32_t)((rows + rows_of_wg - 1) / rows_of_wg);
   s.suffix_blocks = (int32_t)((ratio + kRowsTile - 1) / kRowsTile);
   s.suffix_chunk = chunk(s.max_suffix, (int64_t)a.n_seqs * cache.n_kv_heads * s.suffix_blocks, 1024);
-  s.prefix_chunk = chunk(s.max_prefix, (int64_t)a.n_groups * cache.n_kv_heads * s.prefix_blocks, 256);
+  s.prefix_chunk = chunk(s.max_prefix, (int64_t)a.n_groups * cache.n_kv_heads * s.prefix_blocks, two ? 256 : 1024);
   s.suffix_parts = std::max(1, (s.max_suffix + s.suffix_chunk - 1) / s.suffix_chunk);
   s.prefix_parts = rows ? (s.max_prefix + s.prefix_chunk - 1) / s.prefix_chunk : 0;
+  if (s.prefix_parts == 0) s.row_waves = 0;
   s.direct = s.prefix_parts == 0 && s.suffix_parts == 1;
   const uint64_t items = (uint64_t)a.n_groups * s.prefix_parts * cache.n_kv_heads;
   s.prefix_wgs = (items + 7) / 8 * 8 * s.prefix_blocks;
   s.suffix_wgs = (uint64_t)a.n_seqs * s.suffix_parts * s.suffix_blocks * cache.n_kv_heads;
+  // where more workgroups than the chip holds at a time have lengths of their own (above: 94 us, 107 in the order of the sequences; 165 against 164 where all are alike)
+  s.ordered = a.n_seqs <= kThreads && s.suffix_wgs > 3 * 256;
   if (!s.direct) s.workspace = ((size_t)a.n_seqs * a.n_q_heads * (s.prefix_parts + s.suffix_parts)) * (cache.head_dim + 2) * sizeof(float);
   return s;
 }

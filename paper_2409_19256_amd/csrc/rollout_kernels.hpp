@@ -30,10 +30,11 @@ struct AttendShape {
   int32_t max_prefix, max_suffix;     // tokens, cut to what the tables can name
   int32_t prefix_chunk, suffix_chunk; // tokens of one part, multiples of 128
   int32_t prefix_parts, suffix_parts; // parts of the longest prompt and response
-  int32_t q_tiles, row_waves;         // for prompts: 16-row query tiles of a wavefront, wavefronts of a workgroup with rows of their own
+  int32_t row_waves;                  // prompts with more than 16 rows to a KV head: wavefronts of a workgroup that have rows of their own (32 each); 0 = no such
   bool lanes;                         // pages too small (or tokens too far apart) for addresses that a wavefront shares
   int32_t prefix_blocks, suffix_blocks; // query blocks
   bool direct;                        // one part a row: no merge
+  bool ordered;                       // the longest responses first
   uint64_t prefix_wgs, suffix_wgs;
   size_t workspace;
 };

@@ -194,6 +194,11 @@ ATTENTIONS = [
     ("bf16", 3, 1, 200, 8, "heads", 5, (2,), (35,), (20, 40)),
     ("f16", 1, 1, 1, 4, "heads", 0, (1,), (5,), (2,)),
     ("bf16", 32, 1, 128, 64, "heads", 0, (17,), (257,), (0, 1, 2)),           # one KV head, 544 rows to the prompt
+    ("f16", 24, 8, 64, 32, "heads", 0, (60, 55), (95, 130), (3, 150, 40, 40, 0, 97)),  # more workgroups than the chip holds: longest first
+    ("bf16", 8, 8, 32, 8, "tokens", 0, (4,) * 25, (20, 33), (1, 70, 35)),
+    ("bf16", 8, 8, 64, 16, "heads", 0, (130, 140), (7,), (11, 3)),            # more sequences than a workgroup orders
+    ("f16", 8, 2, 128, 16, "heads", 0, (5, 2, 4), (300, 1, 129), (600, 0, 290)),  # 20 rows
+    ("bf16", 16, 2, 64, 4, "heads", 0, (12, 3), (150, 400), (10, 300)),       # 96 rows
 ]
 
 
