@@ -330,18 +330,18 @@ template <int kN, int kMode> __device__ __forceinline__ void write_part(const At
   if (d0 == 0) p.part_ml[2 * slot] = top == -INFINITY ? -INFINITY : m2, p.part_ml[2 * slot + 1] = sum;
 }
 
+template <typename T, int kN, int kMode>
+__device__ __forceinline__ void write_result(const AttendParams &p, int seq, int head, int part_index, int d0, float top, float scale2, float sum, const float *acc) {
+  if (p.s.direct) write_row<T, kN, kMode>(p, seq, head, d0, top * scale2, sum, acc);
+  else write_part<kN, kMode>(p, ((int64_t)seq * p.a.n_q_heads + head) * (p.s.prefix_parts + p.s.suffix_parts) + part_index, d0, top, top * scale2, sum, acc);
+}
+
 // The parts of a workgroup's wavefronts become one: kRowWaves of them have rows of their own, the others the same rows over other tokens.
 template <typename T, int kDim, int kWaves, int kQ, int kRowWaves, int kMode>
 __device__ __forceinline__ void join_waves(const AttendParams &p, Rows<T, kDim / 16> (&r)[kQ], Members who, int row0, int kv_head, int part_index, float scale2, float *shared) {
   constexpr int kOwn = kDim / 16, kTokenWaves = kWaves / kRowWaves;
   const int rows = who.n * p.ratio, col = threadIdx.x % 16, grp = threadIdx.x % kWave / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
-  const auto write = [&](int row, int d0, float top, float sum, const float *acc) {
-    const int seq = who.first + row / p.ratio, head = kv_head * p.ratio + row % p.ratio;
-    if (p.s.direct) write_row<T, kOwn, kMode>(p, seq, head, d0, top * scale2, sum, acc);
-    else write_part<kOwn, kMode>(p, ((int64_t)seq * p.a.n_q_heads + head) * (p.s.prefix_parts + p.s.suffix_parts) + part_index, d0, top, top * scale2, sum, acc);
-  };
-
 #pragma unroll
   for (int n = 0; n < kQ; ++n) r[n].l = over_rows<Sum>(r[n].l);
   constexpr int kPitch = kDim + 4, kRows = kRowWaves * kRowsTile;
@@ -371,7 +371,7 @@ __device__ __forceinline__ void join_waves(const AttendParams &p, Rows<T, kDim /
 #pragma unroll
           for (int e = 0; e < kOwn; ++e) acc[e] += weight * shared[(w * kRows + at) * kPitch + d0 + e];
         }
-        write(row, d0, top, sum, acc);
+        write_result<T, kOwn, kMode>(p, who.first + row / p.ratio, kv_head * p.ratio + row % p.ratio, part_index, d0, top, scale2, sum, acc);
       }
     }
   }
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(kWaves * kWave, kDim > 128 || kMode == kElements ? 
     const int row0 = block * kRowWaves * kQ * kRowsTile;
     if (begin >= end || row0 >= who.n * p.ratio) return;
     part<T, kDim, kWaves, kQ, kRowWaves, kMode, kLanes, kOnce>(p, a.prefix_pages + (int64_t)g * a.prefix_width, begin, end, who, row0, kv_head, index, shared);
-  } else if constexpr (kQ * kRowWaves == 1) {
+  } else {
     id -= prefix_wgs;
     const int kv_head = id % p.n_kv_heads;
     id /= p.n_kv_heads;
@@ -489,6 +489,53 @@ __global__ __launch_bounds__(kWaves * kWave, kDim > 128 || kMode == kElements ? 
     if (begin >= end && !p.s.direct) return;
     part<T, kDim, kWaves, 1, 1, kMode, kLanes, kOnce>(p, a.suffix_pages + (int64_t)seq * a.suffix_width, begin, end, Members{seq, 1}, block * kRowsTile, kv_head,
                                                       p.s.prefix_parts + index, shared);
+  }
+}
+
+// Responses so short, and so many, that a workgroup for each would do little but start up: a wavefront takes one sequence and KV head, all of its tokens.
+template <typename T, int kDim, int kMode, bool kLanes> __global__ __launch_bounds__(kThreads, kDim > 128 || kMode == kElements ? 1 : kDim > 64 ? 2 : 3)
+void attend_short(AttendParams p) {
+  typedef Reader<T, kDim, kMode, kLanes, true> R;
+  constexpr int kSteps = R::kSteps, kOwn = R::kOwn;
+  const hf_attention &a = p.a;
+  uint32_t id = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int kv_head = id % p.n_kv_heads;
+  id /= p.n_kv_heads;
+  const int row0 = id % p.s.suffix_blocks * kRowsTile, seq = id / p.s.suffix_blocks;
+  if (seq >= a.n_seqs) return;
+  const int end = min(load_scalar(a.suffix_lens + seq), p.s.max_suffix);
+  if (end <= 0 && !p.s.direct) return;
+  const R reader = {p};
+  const int32_t *table = a.suffix_pages + (int64_t)seq * a.suffix_width;
+  u32x4 q[kSteps];
+  Rows<T, kOwn> r;
+  reader.load_queries(q, seq, row0 + reader.col, p.ratio, kv_head);
+  r.clear();
+  for (int token = 0; token < end; token += kTile) {
+    u32x4 k[2][kSteps];
+    uint32_t v[8][kOwn / 2];
+    const typename R::At at = reader.place(reader.pages_at(table, token, end), token, kv_head);
+    reader.load_keys(k, at);
+    reader.load_values(v, at);
+    bool seen[8];
+    const bool whole = reader.visible(seen, at, token, end);
+    f32x4 s[2];
+    R::scores(s, k, q);
+    u32x4 hi, lo;
+    r.join(s, whole, seen, reader.scale2, hi, lo);
+    if (!whole) R::blank(v, seen);
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) r.add(j, R::turned(v, j), hi, lo);
+  }
+  const float sum = over_rows<Sum>(r.l);
+  const int row = row0 + reader.col;
+  if (row >= p.ratio) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float acc[kOwn];
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) acc[j] = r.o[j][i];
+    write_result<T, kOwn, kMode>(p, seq, kv_head * p.ratio + row, p.s.prefix_parts, kOwn * (4 * reader.grp + i), r.m, reader.scale2, sum, acc);
   }
 }
 
@@ -568,19 +615,24 @@ template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void atte
 
 template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, hipStream_t st) {
   const AttendShape &s = p.s;
-  uint32_t prefix_wgs = (uint32_t)s.prefix_wgs;
+  uint32_t prefix_wgs = (uint32_t)s.prefix_wgs, suffix_wgs = (uint32_t)s.suffix_wgs;
   hipError_t e = hipSuccess;
   if constexpr (kDim <= 128 && kMode != kElements) {
     if (s.row_waves) {
-      const dim3 grid(prefix_wgs);
-      e = s.row_waves == 4   ? enqueue_kernel(attend_parts<T, kDim, 8, 2, 4, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs)
-          : s.row_waves == 2 ? enqueue_kernel(attend_parts<T, kDim, 8, 2, 2, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs)
-                             : enqueue_kernel(attend_parts<T, kDim, 8, 2, 1, kMode, kLanes, false>, grid, 8 * kWave, st, p, prefix_wgs);
+      const auto prompts = [&](auto kernel) { return enqueue_kernel(kernel, dim3(prefix_wgs + (s.together ? suffix_wgs : 0)), 8 * kWave, st, p, prefix_wgs); };
+      e = s.row_waves == 4   ? prompts(attend_parts<T, kDim, 8, 2, 4, kMode, kLanes, false>)
+          : s.row_waves == 2 ? prompts(attend_parts<T, kDim, 8, 2, 2, kMode, kLanes, false>)
+                             : prompts(attend_parts<T, kDim, 8, 2, 1, kMode, kLanes, false>);
       prefix_wgs = 0;
+      if (s.together) suffix_wgs = 0;
     }
   }
-  if (e == hipSuccess)
-    e = enqueue_kernel(attend_parts<T, kDim, 4, 1, 1, kMode, kLanes, true>, dim3((uint32_t)(prefix_wgs + s.suffix_wgs)), 4 * kWave, st, p, prefix_wgs);
+  if (s.brief) {
+    if (e == hipSuccess && prefix_wgs) e = enqueue_kernel(attend_parts<T, kDim, 4, 1, 1, kMode, kLanes, true>, dim3(prefix_wgs), 4 * kWave, st, p, prefix_wgs);
+    if (e == hipSuccess) e = enqueue_kernel(attend_short<T, kDim, kMode, kLanes>, dim3((suffix_wgs + 3) / 4), kThreads, st, p);
+  } else if (e == hipSuccess && prefix_wgs + suffix_wgs) {
+    e = enqueue_kernel(attend_parts<T, kDim, 4, 1, 1, kMode, kLanes, true>, dim3(prefix_wgs + suffix_wgs), 4 * kWave, st, p, prefix_wgs);
+  }
   if (e != hipSuccess || s.direct) return e;
   const int64_t rows = (int64_t)p.a.n_seqs * p.a.n_q_heads;
   constexpr int kTeams = kThreads / (kDim / 4);
@@ -602,18 +654,33 @@ template <typename T> hipError_t launch_type(const AttendParams &p, bool vec, hi
 
 } // namespace
 
+constexpr uint64_t kResident = 3 * 256; // workgroups of four wavefronts that the chip holds
+
 AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool vec) {
   AttendShape s = {};
   const int64_t page = cache.page_tokens, ratio = a.n_q_heads / cache.n_kv_heads;
   s.max_suffix = (int32_t)std::min<int64_t>(a.max_suffix, std::min<int64_t>(a.suffix_width * page, 1 << 30));
   s.max_prefix = a.n_groups ? (int32_t)std::min<int64_t>(a.max_prefix, std::min<int64_t>(a.prefix_width * page, 1 << 30)) : 0;
-  // Parts are as long as they may be while there are `want` workgroups.  A workgroup starts up for some 5 us (length, page numbers, first tiles one after another) and
+  // Parts are as long as they may be while there are 1024 workgroups.  A workgroup starts up for some 5 us (length, page numbers, first tiles one after another) and
   // every part costs its rows a partial result.  us at 1 / 2 / 4 / 8 parts a response, 128 responses of 2048 tokens (8 KV heads, eight rows each) 165 / 178 /
-  // 198 / 237, of 1 to 2048 tokens 94 / 104 / 114 / 140; prompts with 128 rows (8, of 2048) at 128 / 256 / 512 workgroups 48 / 32 / 40, with 488 (one, of 32749) 84 / 52 / 61.
-  const auto chunk = [&](int64_t len, int64_t others, int64_t want) {
+  // 198 / 237, of 1 to 2048 tokens 94 / 104 / 114 / 140.
+  const auto chunk = [&](int64_t len, int64_t others) {
     int64_t c = 128;
-    while (c < len && others * ((len + 2 * c - 1) / (2 * c)) >= want) c *= 2;
+    while (c < len && others * ((len + 2 * c - 1) / (2 * c)) >= 1024) c *= 2;
     return (int32_t)c;
+  };
+  // Prompts with many rows: a CU holds one workgroup, which takes 12 us and 30 ns a token of 128 rows (half of that for every half of the rows), and a part costs a row 0.26 ns
+  // in writing and merging.  us at 16 / 32 / 64 parts, 488 rows over 32749 tokens 84 / 52 / 61 (the sum says 77 / 51 / 71).
+  const auto chunk_of_prompts = [&](int64_t len, int64_t others, int row_waves) {
+    int64_t best = 0;
+    double least = 0;
+    for (int64_t n = 1; n <= 256; n += n < 16 ? 1 : n / 8) {
+      const int64_t c = std::max<int64_t>((len + n * 128 - 1) / (n * 128) * 128, 128), parts = (len + c - 1) / c;
+      const double us = (double)((others * parts + 255) / 256) * (12 + 0.0075 * row_waves * (double)c) + 2.6e-4 * (double)parts * a.n_seqs * a.n_q_heads;
+      if (best == 0 || us < least) best = c, least = us;
+      if (c == 128) break;
+    }
+    return (int32_t)best;
   };
   const int64_t rows = std::min<int64_t>(a.max_group, a.n_seqs) * ratio;
   const bool two = vec && cache.head_dim <= 128 && rows > kRowsTile;
@@ -622,8 +689,9 @@ AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool v
   const int64_t rows_of_wg = two ? 2 * s.row_waves * kRowsTile : kRowsTile;
   s.prefix_blocks = (int32_t)((rows + rows_of_wg - 1) / rows_of_wg);
   s.suffix_blocks = (int32_t)((ratio + kRowsTile - 1) / kRowsTile);
-  s.suffix_chunk = chunk(s.max_suffix, (int64_t)a.n_seqs * cache.n_kv_heads * s.suffix_blocks, 1024);
-  s.prefix_chunk = chunk(s.max_prefix, (int64_t)a.n_groups * cache.n_kv_heads * s.prefix_blocks, two ? 256 : 1024);
+  s.suffix_chunk = chunk(s.max_suffix, (int64_t)a.n_seqs * cache.n_kv_heads * s.suffix_blocks);
+  const int64_t prompts = (int64_t)a.n_groups * cache.n_kv_heads * s.prefix_blocks;
+  s.prefix_chunk = two ? chunk_of_prompts(s.max_prefix, prompts, s.row_waves) : chunk(s.max_prefix, prompts);
   s.suffix_parts = std::max(1, (s.max_suffix + s.suffix_chunk - 1) / s.suffix_chunk);
   s.prefix_parts = rows ? (s.max_prefix + s.prefix_chunk - 1) / s.prefix_chunk : 0;
   if (s.prefix_parts == 0) s.row_waves = 0;
@@ -632,7 +700,9 @@ AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool v
   s.prefix_wgs = (items + 7) / 8 * 8 * s.prefix_blocks;
   s.suffix_wgs = (uint64_t)a.n_seqs * s.suffix_parts * s.suffix_blocks * cache.n_kv_heads;
   // where more workgroups than the chip holds at a time have lengths of their own (above: 94 us, 107 in the order of the sequences; 165 against 164 where all are alike)
-  s.ordered = a.n_seqs <= kThreads && s.suffix_wgs > 3 * 256;
+  s.ordered = a.n_seqs <= kThreads && s.suffix_wgs > kResident && s.max_suffix > 4 * kTile * 4;
+  s.brief = s.suffix_wgs > kResident && s.max_suffix <= 4 * kTile;
+  s.together = s.row_waves && !s.brief && s.suffix_wgs <= 256;
   if (!s.direct) s.workspace = ((size_t)a.n_seqs * a.n_q_heads * (s.prefix_parts + s.suffix_parts)) * (cache.head_dim + 2) * sizeof(float);
   return s;
 }

@@ -35,6 +35,8 @@ struct AttendShape {
   int32_t prefix_blocks, suffix_blocks; // query blocks
   bool direct;                        // one part a row: no merge
   bool ordered;                       // the longest responses first
+  bool brief;                         // a wavefront, not a workgroup, for a response and KV head
+  bool together;                      // responses in the grid of the prompts with many rows
   uint64_t prefix_wgs, suffix_wgs;
   size_t workspace;
 };

@@ -199,6 +199,9 @@ ATTENTIONS = [
     ("bf16", 8, 8, 64, 16, "heads", 0, (130, 140), (7,), (11, 3)),            # more sequences than a workgroup orders
     ("f16", 8, 2, 128, 16, "heads", 0, (5, 2, 4), (300, 1, 129), (600, 0, 290)),  # 20 rows
     ("bf16", 16, 2, 64, 4, "heads", 0, (12, 3), (150, 400), (10, 300)),       # 96 rows
+    ("bf16", 32, 8, 64, 16, "heads", 0, (70, 40), (33,), (0, 1, 31, 64, 33, 97, 128)),  # a wavefront to a short response
+    ("f16", 20, 10, 72, 8, "tokens", 0, (1,) * 90, (40, 0), (5, 0, 128)),
+    ("bf16", 40, 2, 48, 16, "heads", 0, (200,), (9,), (7, 33)),               # and 20 query heads to a KV head
 ]
 
 
@@ -229,7 +232,7 @@ def test_attention(case):
 @pytest.mark.parametrize("dtype,by", [("bf16", "heads"), ("f16", "tokens")])
 def test_attention_without_prompts(dtype, by):
     gen = torch.Generator("cuda").manual_seed(3)
-    for lens in ((0, 1, 5, 128), (129, 3, 500, 0), (1,), (0,)):
+    for lens in ((0, 1, 5, 128), (129, 3, 500, 0), (1,), (0,), (100, 3, 0) * 150):
         say("[attend without prompts]", dtype, by, lens)
         c, q, (sl, st, *_), n = attention_inputs(gen, dtype, 8, 2, 128, 16, by, 0, [len(lens)], (0,), lens)
         got = c.attend(q, sl, st)
