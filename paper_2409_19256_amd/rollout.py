@@ -97,7 +97,9 @@ class KvCache:
             qp, q0, q1 = _rows(q, "q", dtype, shape)
             if q_out is None:
                 q_out = torch.empty(shape, dtype=dtype, device=q.device)
-            op, o0, o1 = _rows(q_out, "q_out", dtype, shape)
+                op, o0, o1 = q_out.data_ptr(), n_q * dim, dim
+            else:
+                op, o0, o1 = _rows(q_out, "q_out", dtype, shape)
         cp = sp = pp = rot = table = 0
         if cos is not None:
             table, pairs = cos.shape
@@ -125,9 +127,14 @@ class KvCache:
         qp, q0, q1 = _rows(q, "q", dtype, shape)
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=dev)
-        op, o0, o1 = _rows(out, "out", dtype, shape)
+            op, o0, o1 = out.data_ptr(), heads * dim, dim
+        else:
+            op, o0, o1 = _rows(out, "out", dtype, shape)
         if lse is None:
             lse = torch.empty((n, heads), dtype=torch.float32, device=dev)
+            sp = lse.data_ptr()
+        else:
+            sp = _whole(lse, "lse", torch.float32, (n, heads))
         groups = width = gp = lp = pp = 0
         if group_offsets is not None:
             groups, width = prefix_pages.shape
@@ -135,7 +142,7 @@ class KvCache:
             lp = _whole(prefix_lens, "prefix_lens", torch.int32, (groups,))
             pp = _whole(prefix_pages, "prefix_pages", torch.int32, (groups, width))
         own = suffix_pages.shape[1]
-        pointers = (qp, op, _whole(lse, "lse", torch.float32, (n, heads)), _whole(suffix_lens, "suffix_lens", torch.int32, (n,)),
+        pointers = (qp, op, sp, _whole(suffix_lens, "suffix_lens", torch.int32, (n,)),
                     _whole(suffix_pages, "suffix_pages", torch.int32, (n, own)), gp, lp, pp)
         rest = (q0, q1, o0, o1, n, heads, groups, n if max_group is None else max_group, width, own,
                 width * page if max_prefix is None else max_prefix, own * page if max_suffix is None else max_suffix,
