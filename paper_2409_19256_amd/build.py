@@ -5,12 +5,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhfreshard.so")
 BENCH_EXE = os.path.join(PKG, "hfbench")
+TORCH_MODULE = os.path.join(PKG, "_rollout.so")
 SOURCES = ["planner.cpp", "reshard_kernels.hip", "abi.hip", "append_kernels.hip", "attend_kernels.hip", "logprob_kernels.hip", "rollout_abi.hip"]
 
 
@@ -43,7 +45,29 @@ def build_library(verbose: bool = True) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True, cwd=ROOT)
     os.replace(BENCH_EXE + ".tmp", BENCH_EXE)
+    build_torch_module(verbose)
     return LIB
+
+
+def build_torch_module(verbose: bool = True) -> None:
+    """rollout.py's native part: host code over torch's headers, linked against the library.  Without torch there is nothing to build it for."""
+    try:
+        import torch
+        from torch.utils.cpp_extension import include_paths, library_paths
+    except ImportError:
+        return
+    cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", os.path.join(ROOT, "include")]
+    for path in include_paths() + [sysconfig.get_paths()["include"]]:
+        cmd += ["-isystem", path]
+    cmd += [os.path.join(CSRC, "rollout_torch.cpp"), "-o", TORCH_MODULE + ".tmp", "-L", PKG, "-lhfreshard", "-Wl,-rpath,$ORIGIN"]
+    for path in library_paths():
+        cmd += ["-L", path]
+    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True, cwd=ROOT)
+    os.replace(TORCH_MODULE + ".tmp", TORCH_MODULE)
 
 
 if __name__ == "__main__":
