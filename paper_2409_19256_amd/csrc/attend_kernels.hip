@@ -25,6 +25,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lanes.hpp"
 #include "rollout_kernels.hpp"
@@ -409,15 +410,15 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
     typename R::Pages next = reader.pages_at(table, token + kStep, end);
     reader.load_keys(k, at);
     reader.load_values(v, at);
-    for (;;) {
-      const bool more = token + kStep < end;
+    // (the last tile has code of its own: with a branch around the loads the compiler could not tell how many are on their way, and would wait for all)
+    const auto turn = [&](auto more) {
       bool seen[8];
       const bool whole = reader.visible(seen, at, token, end);
       f32x4 s[kQ][2];
 #pragma unroll
       for (int n = 0; n < kQ; ++n) R::scores(s[n], k, q[n]);
-      at = reader.place(next, token + kStep, kv_head);
-      if (more) {
+      if constexpr (more) {
+        at = reader.place(next, token + kStep, kv_head);
         next = reader.pages_at(table, token + 2 * kStep, end);
         reader.load_keys(k, at);
       }
@@ -431,10 +432,10 @@ __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table
 #pragma unroll
         for (int n = 0; n < kQ; ++n) r[n].add(j, left, hi[n], lo[n]);
       }
-      token += kStep;
-      if (!more) break;
-      reader.load_values(v, at);
-    }
+      if constexpr (more) reader.load_values(v, at);
+    };
+    for (; token + kStep < end; token += kStep) turn(std::true_type());
+    turn(std::false_type());
   }
 
   join_waves<T, kDim, kWaves, kQ, kRowWaves, kMode>(p, r, who, row0, kv_head, part_index, scale2, shared);

@@ -4,8 +4,9 @@
 //   dx_j = ([j = t] g - p_j (g + h (ln p_j + H))) / temperature
 //
 // The forward pass reads every logit once and writes a few numbers a row; the gradient reads and writes each once.  HBM is
-// the bound: at 2 bytes an element there is room for about fourteen vector operations on each, and the forward pass needs nine (a base-2
-// exponential counts as four).  A workgroup takes a row; every lane keeps its own running maximum, sum and weighted sum over its vectors and
+// the bound of the gradient (6.2 TB/s at 4096 x 32000 bf16, read and written) and of 32-bit logits (5.6 TB/s at 2048 x 128256).  At 2 bytes an element the forward pass has
+// room for eleven vector operations on each and needs nine and a half (a base-2 exponential counts as four): 4.9 TB/s at 4096 x 32000, where the issue slots are
+// nearly full.  A workgroup takes a row; every lane keeps its own running maximum, sum and weighted sum over its vectors and
 // they are merged once at the end.
 //
 // The likeliest tokens come out of the same pass: besides its maximum a lane remembers in which of its vectors it first met it.
@@ -62,31 +63,49 @@ __device__ __forceinline__ int64_t target_of(const Logits &in, int64_t row) {
   return in.target_bytes == 8 ? static_cast<const int64_t *>(in.targets)[row] : static_cast<const int32_t *>(in.targets)[row];
 }
 
-// Largest element m, and sums over the elements of 2^d and of 2^d d with d = x c - k, c = log2(e) / temperature.  k is m c rounded to a whole number: then d
-// is one operation, with one rounding, and sums move to another k exactly, where m c itself would be off by as much as its own rounding.
+// The larger ones; fmaxf would first make a quiet NaN of what might be a signalling one, an operation for every element.
+__device__ __forceinline__ float larger(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float larger(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// Largest element m, and sums over the elements of 2^d and of 2^d d with d = x c - k, c = log2(e) / temperature.  k is x0 c rounded to a whole number: then d
+// is one operation, with one rounding, and sums move to another k exactly, where x0 c itself would be off by as much as its own rounding.  x0 is
+// the largest element of a lane's first vectors and follows m only when that is past it by kSlack of base 2, which for most lanes never happens.
 struct Stats {
-  float m, k, s, u;
+  float m, x0, k, s, u;
 };
-__device__ __forceinline__ float base_of(float m, float c) { return m == -INFINITY ? 0.f : rintf(m * c); }
-// to a larger maximum
-__device__ __forceinline__ void rebase(Stats &st, float m, float c) {
-  const float k = base_of(m, c);
-  float d = st.k - k; // m c past the largest float: from maximum to maximum (see join)
-  if (d != d) d = (st.m - m) * c;
-  if (st.m == -INFINITY) d = 0; // before the first element there is nothing to move
+constexpr float kSlack = 8;
+__device__ __forceinline__ void rebase(Stats &st, float x0, float c) {
+  const float k = x0 == -INFINITY ? 0.f : rintf(x0 * c);
+  float d = st.k - k; // x0 c past the largest float: from element to element (see join)
+  if (d != d) d = (st.x0 - x0) * c;
+  if (st.x0 == -INFINITY) d = 0; // before the first element there is nothing to move
   const float down = __builtin_amdgcn_exp2f(d);
   st.u = st.s > 0 ? down * fmaf(fmaxf(d, -200.f), st.s, st.u) : st.u;
   st.s *= down;
-  st.m = m;
+  st.x0 = x0;
   st.k = k;
 }
 __device__ __forceinline__ Stats merge_wave(Stats st, float c) {
-  rebase(st, over_wave<Max>(st.m), c);
-  return {st.m, st.k, over_wave<Sum>(st.s), over_wave<Sum>(st.u)};
+  st.m = over_wave<Max>(st.m);
+  rebase(st, st.m, c);
+  return {st.m, st.x0, st.k, over_wave<Sum>(st.s), over_wave<Sum>(st.u)};
 }
 
-template <int kN> __device__ __forceinline__ void join(Stats &st, const float (&x)[kN], float top, float c) {
-  if (top > st.m) rebase(st, top, c);
+// limit: x0 and the slack
+template <int kN> __device__ __forceinline__ void join(Stats &st, float &limit, const float (&x)[kN], float top, float c) {
+  st.m = larger(st.m, top);
+  if (top > limit) {
+    rebase(st, top, c);
+    limit = top + kSlack / c;
+  }
   const auto add = [&](float d) {
     const float e = __builtin_amdgcn_exp2f(d); // NaN comes through here
     st.s += e;
@@ -97,7 +116,7 @@ template <int kN> __device__ __forceinline__ void join(Stats &st, const float (&
     for (int i = 0; i < kN; ++i) add(fmaf(x[i], c, -st.k));
   } else {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) add((x[i] - st.m) * c);
+    for (int i = 0; i < kN; ++i) add((x[i] - st.x0) * c);
   }
 }
 
@@ -160,7 +179,8 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
   const float x_target = (float)row[target];
   const float c = in.inv_temperature * kLog2e;
   const int n_vec = vocab / kV; // whole ones
-  Stats st = {-INFINITY, 0, 0, 0};
+  Stats st = {-INFINITY, -INFINITY, 0, 0, 0};
+  float limit = -INFINITY;
   float best = -INFINITY;         // the lane's largest element
   uint32_t best_at = 0xFFFFFFFFu; // and the vector that had it first; none: no vectors
   if constexpr (kTop) {
@@ -175,11 +195,11 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
 #pragma unroll
-      for (int e = 0; e < kV; ++e) {
-        x[k * kV + e] = (float)v[k][e];
-        tops[k] = e ? fmaxf(tops[k], x[k * kV + e]) : x[k * kV + e];
-      }
-      top = k ? fmaxf(top, tops[k]) : tops[k];
+      for (int e = 0; e < kV; ++e) x[k * kV + e] = (float)v[k][e];
+      tops[k] = larger(x[k * kV], x[k * kV + 1]);
+#pragma unroll
+      for (int e = 2; e < kV; e += 2) tops[k] = larger(tops[k], x[k * kV + e], x[k * kV + e + 1]);
+      top = k ? larger(top, tops[k]) : tops[k];
     }
     if constexpr (kTop)
       if (top > best || best_at == 0xFFFFFFFFu) {
@@ -190,7 +210,7 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
           if (tops[k] == top) best_at = at + k * kThreads;
         if (tops[0] == top) best_at = at;
       }
-    join(st, x, top, c);
+    join(st, limit, x, top, c);
   };
   // the next vectors are on their way while the present ones are added
   int i = t;
@@ -206,15 +226,14 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
       }
     };
     load_batch(v, i);
-    for (;;) {
-      const int at = i;
-      i += kBatch * kThreads;
-      const bool more = i + (kBatch - 1) * kThreads < n_vec;
-      if (more) load_batch(next, i);
-      add(v, at);
-      if (!more) break;
+    // (no branch around the loads: the compiler could not tell how many are on their way, and would wait for all)
+    for (; i + (2 * kBatch - 1) * kThreads < n_vec; i += kBatch * kThreads) {
+      load_batch(next, i + kBatch * kThreads);
+      add(v, i);
       for (int k = 0; k < kBatch; ++k) v[k] = next[k];
     }
+    add(v, i);
+    i += kBatch * kThreads;
   }
   { // fewer than kBatch are left, and the vector that the row ends in
     V v[kBatch - 1];
@@ -242,7 +261,9 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
     if (lane == 0) stats[wave] = st;
   }
   if constexpr (kWaves > 1 || kTop) __syncthreads();
-  if constexpr (kWaves > 1) st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, 0, 0, 0}, c);
+  if constexpr (!kTop)
+    if (wave > 0) return; // the rest is a few numbers
+  if constexpr (kWaves > 1) st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, -INFINITY, 0, 0, 0}, c);
   // of base e: lse = top + log_z
   const float top = st.m == -INFINITY ? 0.f : st.m * in.inv_temperature, log2_s = __builtin_amdgcn_logf(st.s);
   const float past = st.m == -INFINITY || !(fabsf(st.k) < INFINITY) ? 0.f : fmaf(st.m, c, -st.k), log_z = (log2_s - past) * kLn2;
@@ -297,7 +318,8 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
     }
     __syncthreads();
     const uint32_t n = n_found;
-    if (n > kCandidates) return find_by_rounds<T, kThreads>(row, vocab, out.top_n, logprob_of, ids, values, found);
+    // fewer than top_n: a signalling NaN was somebody's largest element
+    if (n > kCandidates || n < (uint32_t)out.top_n) return find_by_rounds<T, kThreads>(row, vocab, out.top_n, logprob_of, ids, values, found);
     for (uint32_t k = t; k < n; k += kThreads) { // ranked by counting: all keys differ
       const uint64_t key = found[k];
       int rank = 0;
@@ -354,7 +376,7 @@ template <typename T> __global__ __launch_bounds__(kBackThreads) void token_logp
 }
 
 // The forward pass reads plainly up to 512 MiB, so that the memory-side cache (256 MiB) keeps what it can for the gradient.  us, plain /
-// non-temporal: 4096 x 32000 bf16 forward then gradient 41 + 71 / 38 + 88 (forward alone 40 / 36), 2048 x 128256 f32 forward 188 / 183.
+// non-temporal, when this was chosen: 4096 x 32000 bf16 forward then gradient 41 + 71 / 38 + 88 (forward alone 40 / 36), 2048 x 128256 f32 forward 188 / 183.
 Logits logits_of(const hf_logits &in) {
   const bool once = in.rows * (int64_t)in.vocab * (in.dtype == HF_F32 ? 4 : 2) > (int64_t)512 << 20;
   return {in.logits, in.targets, in.row_stride, in.vocab, in.target_bytes, in.inv_temperature, once};
@@ -366,9 +388,9 @@ template <typename T, int kThreads> hipError_t launch_threads(const hf_logits &i
   return enqueue_kernel(token_logprobs<T, kThreads, false>, grid, kThreads, st, logits_of(in), out);
 }
 template <typename T> hipError_t launch(const hf_logits &in, const hf_logprobs &out, hipStream_t st) {
-  // Lanes for a row, by its vectors: few rows in flight at a time are better for memory, but a lane wants a few vectors.  us at 64 / 256 / 512 / 1024 lanes:
-  // 1361 x 5004 f16 (625 vectors) 7.6 / 7.8 / 7.8 / 11.3, 64 x 32000 bf16 with alternatives (4000) 20.7 / 9.6 / 8.9 / 8.9, 4096 x 32000 42 / 40 / 39 / 47,
-  // 2048 x 128256 f32 with alternatives (32064) 546 / 256 / 218 / 189.
+  // Lanes for a row, by its vectors: few rows in flight at a time are better for memory, but a lane wants a few vectors (what a wavefront does once a row is worth 40
+  // elements a lane).  us at 64 / 256 / 512 / 1024 lanes: 1361 x 5004 f16 (625 vectors) 7.6 / 7.0 / 7.8 / 11.3, 64 x 32000 bf16 with alternatives (4000) 20.7 / 8.9 / 8.5 /
+  // 8.9, 4096 x 32000 42 / 38 / 36 / 47, 2048 x 128256 f32 with alternatives (32064) 546 / 256 / 218 / 187.
   const int n_vec = in.vocab / kVec<T>;
   if (n_vec <= 512) return launch_threads<T, 64>(in, out, st);
   if (n_vec <= 2048) return launch_threads<T, 256>(in, out, st);

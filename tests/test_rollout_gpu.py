@@ -460,6 +460,22 @@ def test_rows_with_nan_and_infinity(vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("vocab", [50, 5000, 40000])
+def test_rows_with_signalling_nan(vocab):
+    from paper_2409_19256_amd import rollout
+    say("[signalling nan rows]", vocab)
+    x = torch.randn(3, vocab, device="cuda").to(torch.bfloat16)
+    x.view(torch.int16)[0, vocab // 2] = 0x7F81
+    x.view(torch.int16)[1] = 0x7F81
+    x.view(torch.int16)[2, 7::9] = -0x7F  # with its sign
+    got = rollout.token_logprobs(x, torch.zeros(3, dtype=torch.int64, device="cuda"), 1.0, 20)
+    torch.cuda.synchronize()
+    assert all(torch.isnan(t).all() for t in (got.logprob, got.entropy, got.lse))
+    ids = got.top_ids.cpu().numpy()
+    assert ((ids >= 0) & (ids < vocab)).all() and all(len(set(r)) == 20 for r in ids.tolist())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("case", SCORES, ids=str)
 def test_gradient(case):
     from paper_2409_19256_amd import rollout
