@@ -494,7 +494,7 @@ HF_API int hf_plan_validate(const hf_plan *plan);
  * (compute_log_prob and compute_loss of Section 4).
  * Conventions: all pointers inside the argument structs are DEVICE pointers of the current HIP device, the structs
  * themselves are host memory and are read before the call returns.  Strides count ELEMENTS, are not negative, and the last
- * dimension is contiguous; data are aligned to their element, everything else to 4 bytes (64-bit integers to 8).  The calls enqueue one or two
+ * dimension is contiguous; data are aligned to their element, everything else to 4 bytes (64-bit integers to 8).  The calls enqueue one to four
  * kernels on hip_stream and return; they never allocate, synchronise or keep anything from one call for the next, so
  * they can be captured into a graph.  Lengths, page numbers, slots, positions and targets are read on the device: an
  * entry outside its range is left out as said below and never leads to an access outside the buffers.  Sums, softmax
@@ -549,7 +549,8 @@ HF_API int hf_append_kv(const hf_kv_cache *cache, const hf_append *args, void *h
  * members of a group past max_group.  A prompt may have any number of samples, a prompt processed by
  * itself is a sequence per token with lengths 1, 2, 3, ... over one table row.
  * workspace: at least hf_attend_workspace_bytes(cache, args) bytes, 16-byte aligned; its contents do not matter and are
- * not kept.  One or two launches. */
+ * not kept.  One launch where contexts are short and few or nothing is cut into parts, else two to four (prompts, responses, their
+ * results put together). */
 typedef struct {
   const void *q; /* [n_seqs, n_q_heads, head_dim], the cache's type */
   void *out;     /* the same shape and type; not q */

@@ -378,67 +378,67 @@ __device__ __forceinline__ void join_waves(const AttendParams &p, Rows<T, kDim /
   }
 }
 
+// What the queries q see in the tokens of a segment, a tile at every kStep tokens from `token` on.
+template <typename R, typename T, int kDim, int kQ>
+__device__ __forceinline__ void sweep(const R &reader, const int32_t *table, int token, int kStep, int end, int kv_head, const u32x4 (&q)[kQ][R::kSteps],
+                                      Rows<T, kDim / 16> (&r)[kQ]) {
+  // Page numbers are fetched two tiles ahead.  The next tile's keys are on their way from when the scores are made, its values from when they are added
+  // up: each is asked for as soon as its registers are free.
+  u32x4 k[2][R::kSteps];
+  uint32_t v[8][R::kOwn / 2];
+  typename R::At at = reader.place(reader.pages_at(table, token, end), token, kv_head);
+  typename R::Pages next = reader.pages_at(table, token + kStep, end);
+  reader.load_keys(k, at);
+  reader.load_values(v, at);
+  // (the last tile has code of its own: with a branch around the loads the compiler could not tell how many are on their way, and would wait for all)
+  const auto turn = [&](auto more) {
+    bool seen[8];
+    const bool whole = reader.visible(seen, at, token, end);
+    f32x4 s[kQ][2];
+#pragma unroll
+    for (int n = 0; n < kQ; ++n) R::scores(s[n], k, q[n]);
+    if constexpr (more) {
+      at = reader.place(next, token + kStep, kv_head);
+      next = reader.pages_at(table, token + 2 * kStep, end);
+      reader.load_keys(k, at);
+    }
+    u32x4 hi[kQ], lo[kQ];
+#pragma unroll
+    for (int n = 0; n < kQ; ++n) r[n].join(s[n], whole, seen, reader.scale2, hi[n], lo[n]);
+    if (!whole) R::blank(v, seen);
+#pragma unroll
+    for (int j = 0; j < R::kOwn; ++j) {
+      const u32x4 left = R::turned(v, j);
+#pragma unroll
+      for (int n = 0; n < kQ; ++n) r[n].add(j, left, hi[n], lo[n]);
+    }
+    if constexpr (more) reader.load_values(v, at);
+  };
+  for (; token + kStep < end; token += kStep) turn(std::true_type());
+  turn(std::false_type());
+}
+
 // Rows row0 .. of a segment (the sequences [first, first + n), all of which see its tokens) over its tokens [begin, end).  kRowWaves wavefronts
 // have kQ * 16 rows each, and the others the same rows over other tokens.
 template <typename T, int kDim, int kWaves, int kQ, int kRowWaves, int kMode, bool kLanes, bool kOnce>
 __device__ __forceinline__ void part(const AttendParams &p, const int32_t *table, int begin, int end, Members who, int row0, int kv_head, int part_index,
                                      float *shared) {
   typedef Reader<T, kDim, kMode, kLanes, kOnce> R;
-  constexpr int kSteps = R::kSteps, kOwn = R::kOwn, kTokenWaves = kWaves / kRowWaves;
+  constexpr int kTokenWaves = kWaves / kRowWaves;
   const R reader = {p};
-  const int col = reader.col;
-  const float scale2 = reader.scale2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
   const int rows = who.n * p.ratio, my_row0 = row0 + row_wave * kQ * kRowsTile;
 
-  u32x4 q[kQ][kSteps];
-  Rows<T, kOwn> r[kQ];
+  u32x4 q[kQ][R::kSteps];
+  Rows<T, R::kOwn> r[kQ];
 #pragma unroll
   for (int n = 0; n < kQ; ++n) {
-    reader.load_queries(q[n], who.first, my_row0 + n * kRowsTile + col, rows, kv_head);
+    reader.load_queries(q[n], who.first, my_row0 + n * kRowsTile + reader.col, rows, kv_head);
     r[n].clear();
   }
-
-  // Page numbers are fetched two tiles ahead.  The next tile's keys are on their way from when the scores are made, its values from when they are added
-  // up: each is asked for as soon as its registers are free.
-  constexpr int kStep = kTokenWaves * kTile;
-  int token = begin + token_wave * kTile;
-  if (token < end && my_row0 < rows) {
-    u32x4 k[2][kSteps];
-    uint32_t v[8][kOwn / 2];
-    typename R::At at = reader.place(reader.pages_at(table, token, end), token, kv_head);
-    typename R::Pages next = reader.pages_at(table, token + kStep, end);
-    reader.load_keys(k, at);
-    reader.load_values(v, at);
-    // (the last tile has code of its own: with a branch around the loads the compiler could not tell how many are on their way, and would wait for all)
-    const auto turn = [&](auto more) {
-      bool seen[8];
-      const bool whole = reader.visible(seen, at, token, end);
-      f32x4 s[kQ][2];
-#pragma unroll
-      for (int n = 0; n < kQ; ++n) R::scores(s[n], k, q[n]);
-      if constexpr (more) {
-        at = reader.place(next, token + kStep, kv_head);
-        next = reader.pages_at(table, token + 2 * kStep, end);
-        reader.load_keys(k, at);
-      }
-      u32x4 hi[kQ], lo[kQ];
-#pragma unroll
-      for (int n = 0; n < kQ; ++n) r[n].join(s[n], whole, seen, scale2, hi[n], lo[n]);
-      if (!whole) R::blank(v, seen);
-#pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        const u32x4 left = R::turned(v, j);
-#pragma unroll
-        for (int n = 0; n < kQ; ++n) r[n].add(j, left, hi[n], lo[n]);
-      }
-      if constexpr (more) reader.load_values(v, at);
-    };
-    for (; token + kStep < end; token += kStep) turn(std::true_type());
-    turn(std::false_type());
-  }
-
-  join_waves<T, kDim, kWaves, kQ, kRowWaves, kMode>(p, r, who, row0, kv_head, part_index, scale2, shared);
+  const int token = begin + token_wave * kTile;
+  if (token < end && my_row0 < rows) sweep<R, T, kDim, kQ>(reader, table, token, kTokenWaves * kTile, end, kv_head, q, r);
+  join_waves<T, kDim, kWaves, kQ, kRowWaves, kMode>(p, r, who, row0, kv_head, part_index, reader.scale2, shared);
 }
 
 // The sequence with the n-th longest response (equal ones in order), of at most kThreads.  Workgroups are handed out in order: with the longest first
@@ -540,6 +540,44 @@ void attend_short(AttendParams p) {
   }
 }
 
+// Few and short contexts, in one launch: a workgroup takes a sequence and KV head, its wavefronts the tiles of prompt and response in turn.
+// (Eight wavefronts were level or slower: 13.4 against 15.8 us with 512 workgroups of 512 tokens.)
+template <typename T, int kDim, int kMode, bool kLanes>
+__global__ __launch_bounds__(kThreads, kDim > 128 || kMode == kElements ? 1 : 2) void attend_small(AttendParams p) {
+  constexpr int kWaves = kThreads / kWave;
+  typedef Reader<T, kDim, kMode, kLanes, false> R;
+  __shared__ float shared[kWaves * kRowsTile * (kDim + 4 + 2)];
+  const hf_attention &a = p.a;
+  uint32_t id = blockIdx.x;
+  const int kv_head = id % p.n_kv_heads;
+  id /= p.n_kv_heads;
+  const int row0 = id % p.s.suffix_blocks * kRowsTile, seq = id / p.s.suffix_blocks;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const R reader = {p};
+  u32x4 q[1][R::kSteps];
+  Rows<T, R::kOwn> r[1];
+  reader.load_queries(q[0], seq, row0 + reader.col, p.ratio, kv_head);
+  r[0].clear();
+  const int own = min(load_scalar(a.suffix_lens + seq), p.s.max_suffix);
+  int prompt = -1;
+  for (int g0 = 0; g0 < a.n_groups && prompt < 0; g0 += kWave) { // every lane asks for another prompt whether the sequence is one of its samples
+    const int g = g0 + (int)(threadIdx.x % kWave);
+    const Members who = members(a, min(g, a.n_groups - 1));
+    const uint64_t its = __builtin_amdgcn_ballot_w64(g < a.n_groups && seq >= who.first && seq < who.first + who.n);
+    if (its) prompt = g0 + __builtin_ctzll(its);
+  }
+  int tiles = 0;
+  if (prompt >= 0) {
+    const int end = min(load_scalar(a.prefix_lens + prompt), p.s.max_prefix);
+    tiles = max(end + kTile - 1, 0) / kTile;
+    if (wave * kTile < end)
+      sweep<R, T, kDim, 1>(reader, a.prefix_pages + (int64_t)prompt * a.prefix_width, wave * kTile, kWaves * kTile, end, kv_head, q, r);
+  }
+  const int token = (wave + kWaves - tiles % kWaves) % kWaves * kTile; // on with the wavefront whose turn it is
+  if (token < own) sweep<R, T, kDim, 1>(reader, a.suffix_pages + (int64_t)seq * a.suffix_width, token, kWaves * kTile, own, kv_head, q, r);
+  join_waves<T, kDim, kWaves, 1, 1, kMode>(p, r, Members{seq, 1}, row0, kv_head, 0, reader.scale2, shared);
+}
+
 // A row (sequence, query head) out of its parts, in order.  kDim / 4 lanes have four elements of it each; `split` such teams share a row's parts
 // where these are many, each taking every split-th.
 template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void attend_merge(AttendParams p, int split) {
@@ -616,6 +654,9 @@ template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void atte
 
 template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, hipStream_t st) {
   const AttendShape &s = p.s;
+  if (s.small) {
+    return enqueue_kernel(attend_small<T, kDim, kMode, kLanes>, dim3((uint32_t)s.suffix_wgs), kThreads, st, p);
+  }
   uint32_t prefix_wgs = (uint32_t)s.prefix_wgs, suffix_wgs = (uint32_t)s.suffix_wgs;
   hipError_t e = hipSuccess;
   if constexpr (kDim <= 128 && kMode != kElements) {
@@ -705,6 +746,14 @@ AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool v
   s.brief = s.suffix_wgs > kResident && s.max_suffix <= 4 * kTile;
   s.together = s.row_waves && !s.brief && s.suffix_wgs <= 256;
   if (!s.direct) s.workspace = ((size_t)a.n_seqs * a.n_q_heads * (s.prefix_parts + s.suffix_parts)) * (cache.head_dim + 2) * sizeof(float);
+  // (the workspace stays as it is asked for by the parts, so that it follows from those alone)
+  // One launch over whole contexts saves the merge and its launch, and reads a prompt once for every sample, from L2; a workgroup takes 3 us and 9 ns a token of 128
+  // elements.  us, parts / one launch: 16 workgroups (sequence, KV head) of 164 tokens 8.5 / 5.6, 64 of 512 9.7 / 7.9, of 1024 11.5 / 11.9, 32 of 768 9.5 / 10.3, 256 of 1024
+  // 22 / 14, 512 of 1024 23 / 21, 1024 of 512 27 / 23, of 1024 28 / 40, 2048 of 256 35 / 28, of 512 40 / 44; single elements, 64 of 128 17 / 13, of 256 17 / 21.
+  const int64_t tokens = (int64_t)s.max_prefix + s.max_suffix, one = (int64_t)a.n_seqs * s.suffix_blocks * cache.n_kv_heads;
+  const int64_t padded = cache.head_dim <= 64 ? 64 : cache.head_dim <= 128 ? 128 : 256;
+  s.small = !s.direct && tokens <= (vec ? (one < 128 ? 640 : 1024) * 128 / padded : 128) && one * tokens <= 1 << 19;
+  if (s.small) s.direct = true, s.prefix_wgs = 0, s.suffix_wgs = one;
   return s;
 }
 

@@ -33,6 +33,7 @@ struct AttendShape {
   int32_t row_waves;                  // prompts with more than 16 rows to a KV head: wavefronts of a workgroup that have rows of their own (32 each); 0 = no such
   bool lanes;                         // pages too small (or tokens too far apart) for addresses that a wavefront shares
   int32_t prefix_blocks, suffix_blocks; // query blocks
+  bool small;                         // a workgroup for a sequence and KV head, over prompt and response: one launch
   bool direct;                        // one part a row: no merge
   bool ordered;                       // the longest responses first
   bool brief;                         // a wavefront, not a workgroup, for a response and KV head

@@ -229,6 +229,56 @@ def test_attention(case):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("loose", ["prompts", "responses"])
+@pytest.mark.parametrize("case", ATTENTIONS, ids=str)
+def test_attention_within_loose_bounds(case, loose):
+    """Tables with room for far more tokens than there are: work is cut into parts by the bounds, whatever the lengths."""
+    dtype, hq, hk, d, page, by, extra, groups, prefix, suffix = case
+    say("[attend, loose bounds]", loose, case)
+    gen = torch.Generator("cuda").manual_seed(d + 1)
+    c, q, (sl, st, off, pl, pt), n = attention_inputs(gen, dtype, hq, hk, d, page, by, extra, groups, prefix, suffix)
+    room = max(1, 2500 // page)
+    wide = torch.full(((pt if loose == "prompts" else st).shape[0], room), -1, dtype=torch.int32, device="cuda")
+    if loose == "prompts":
+        pt = torch.cat([pt, wide], 1)
+    else:
+        st = torch.cat([st, wide], 1)
+    args = (sl, st, off, pl, pt)
+    got, again = c.attend(q, *args), c.attend(q, *args)
+    torch.cuda.synchronize()
+    check_attention(c, dtype, q, args, got, n)
+    assert torch.equal(bits(got[0]), bits(again[0])) and torch.equal(got[1], again[1])
+
+
+# dtype, query heads, KV heads, head dim, page, samples per prompt, prompt lengths, response lengths: on both sides of where contexts are short and few
+SHORT = [
+    ("bf16", 4, 4, 64, 16, (1,) * 70 + (3,), (33, 0, 64, 95, 128), (0, 1, 31, 32, 33)),
+    ("f16", 2, 1, 128, 16, (2, 2), (31, 32), (0, 96, 97)),
+    ("bf16", 8, 2, 128, 64, (4,), (512,), (128, 127, 1, 0)),
+    ("bf16", 8, 2, 128, 64, (4,), (513,), (128, 127, 1, 0)),
+    ("f16", 16, 8, 128, 16, (16,), (768,), (256, 255)),
+    ("bf16", 6, 2, 256, 8, (3, 2), (256, 255), (64, 0)),
+    ("bf16", 34, 2, 128, 4, (2, 3), (90, 1), (0, 40, 300)),
+    ("f16", 3, 1, 65, 16, (2, 1), (64, 63), (64, 0, 1)),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", SHORT, ids=lambda c: str(c)[:60])
+def test_attention_over_short_contexts(case):
+    dtype, hq, hk, d, page, groups, prefix, suffix = case
+    say("[attend, short contexts]", case)
+    gen = torch.Generator("cuda").manual_seed(d + 2)
+    c, q, args, n = attention_inputs(gen, dtype, hq, hk, d, page, "heads", 0, groups, prefix, suffix)
+    sl, st, off, pl, pt = args
+    for offsets, most in ((off, None), (off + 1, None), (off, 1), (torch.zeros_like(off), None)):  # the last three leave sequences without a prompt
+        args = (sl, st, offsets, pl, pt)
+        got = c.attend(q, *args, **({} if most is None else dict(max_group=most)))
+        torch.cuda.synchronize()
+        check_attention(c, dtype, q, args, got, n, **({} if most is None else dict(max_group=most)))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,by", [("bf16", "heads"), ("f16", "tokens")])
 def test_attention_without_prompts(dtype, by):
     gen = torch.Generator("cuda").manual_seed(3)
