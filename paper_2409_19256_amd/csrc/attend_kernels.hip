@@ -5,14 +5,15 @@
 // Any cut of the tokens into parts gives (m, l, o) of each part, and parts merge exactly:
 // m = max m_i, l = sum l_i exp(m_i - m), o likewise.  A prompt is cut into parts whose rows are all the queries of its samples that
 // read one KV head (samples x query heads per KV head), a response into parts whose rows are the sequence's own query heads, and a
-// second kernel merges a row's parts in a fixed order.
+// second kernel merges a row's parts in a fixed order.  Short contexts are not cut: one workgroup takes prompt and response.
 //
 // Bound: a response's keys and values are read for one sequence alone, 4 bytes per (token, element) for 4 x rows operations, so
 // HBM is the bound there; a prompt's for all of its samples' rows.  What keeps the loads wide and the wavefronts fed:
 //  - a wavefront takes tiles of 32 tokens straight from memory into registers, keys and values of the next tile on their way while it works on
 //    the present one; nothing is staged and no wavefront waits for another until its part is done.  Where a prompt has many
 //    rows, eight wavefronts of a workgroup share its tokens and rows, so that a SIMD has two (prompts brought into LDS by the whole workgroup were
-//    no faster: 54 us where this takes 52, 61 samples of 32749 tokens with 488 rows; it is bound by the vector unit, 41 % of its issue slots);
+//    no faster: 54 us where this takes 51, 61 samples of 32749 tokens with 488 rows; a SIMD issues vector instructions 29 % of that time, its matrix unit
+//    is busy 19 %, and two wavefronts hide no more of each other's waits);
 //  - what is read for one workgroup alone goes past the caches (responses of the 7B shape, 1024 tokens each: 6.8 TB/s, plain loads 6.0);
 //  - a page's number and address are the same for a whole wavefront and are worked out by the scalar unit (pages of 16 tokens and more);
 //  - scores are made transposed, S^T = K Q^T: the accumulator then holds, for the query of a lane's column, four tokens of each 16, which
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(kThreads, kDim > 128 || kMode == kElements ? 1 : 2)
 }
 
 // A row (sequence, query head) out of its parts, in order.  kDim / 4 lanes have four elements of it each; `split` such teams share a row's parts
-// where these are many, each taking every split-th.
+// where these are many, each taking every split-th.  Bound by latency: 3.4 us for 16 rows of two parts, 7.7 for 976 rows of 36, 8.5 for 8192 rows of five.
 template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void attend_merge(AttendParams p, int split) {
   constexpr int kTeam = kDim / 4, kTeams = kThreads / kTeam;
   __shared__ f32x4 shared[kThreads];
@@ -654,9 +655,7 @@ template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void atte
 
 template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, hipStream_t st) {
   const AttendShape &s = p.s;
-  if (s.small) {
-    return enqueue_kernel(attend_small<T, kDim, kMode, kLanes>, dim3((uint32_t)s.suffix_wgs), kThreads, st, p);
-  }
+  if (s.small) return enqueue_kernel(attend_small<T, kDim, kMode, kLanes>, dim3((uint32_t)s.suffix_wgs), kThreads, st, p);
   uint32_t prefix_wgs = (uint32_t)s.prefix_wgs, suffix_wgs = (uint32_t)s.suffix_wgs;
   hipError_t e = hipSuccess;
   if constexpr (kDim <= 128 && kMode != kElements) {
