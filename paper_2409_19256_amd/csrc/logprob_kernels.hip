@@ -78,14 +78,19 @@ __device__ __forceinline__ float larger(float a, float b, float c) {
 // Largest element m, and sums over the elements of 2^d and of 2^d d with d = x c - k, c = log2(e) / temperature.  k is x0 c rounded to a whole number: then d
 // is one operation, with one rounding, and sums move to another k exactly, where x0 c itself would be off by as much as its own rounding.  x0 is
 // the largest element of a lane's first vectors and follows m only when that is past it by kSlack of base 2, which for most lanes never happens.
+// Past kWhole (mask values, low temperatures) the product's own rounding would be a whole number and more: k is infinite there, the
+// base x0 itself, and d = (x - x0) c.
 struct Stats {
   float m, x0, k, s, u;
 };
-constexpr float kSlack = 8;
+constexpr float kSlack = 8, kWhole = 1 << 24;
 __device__ __forceinline__ void rebase(Stats &st, float x0, float c) {
-  const float k = x0 == -INFINITY ? 0.f : rintf(x0 * c);
-  float d = st.k - k; // x0 c past the largest float: from element to element (see join)
-  if (d != d) d = (st.x0 - x0) * c;
+  float k = x0 == -INFINITY ? 0.f : rintf(x0 * c), d = st.k - k;
+  if (!(fmaxf(fabsf(k), st.k) < kWhole)) {
+    const bool was = st.k < INFINITY, is = fabsf(k) < kWhole;
+    d = is ? fmaf(st.x0, c, -k) : was ? -fmaf(x0, c, -st.k) : (st.x0 - x0) * c;
+    if (!is) k = INFINITY;
+  }
   if (st.x0 == -INFINITY) d = 0; // before the first element there is nothing to move
   const float down = __builtin_amdgcn_exp2f(d);
   st.u = st.s > 0 ? down * fmaf(fmaxf(d, -200.f), st.s, st.u) : st.u;
@@ -111,7 +116,7 @@ template <int kN> __device__ __forceinline__ void join(Stats &st, float &limit, 
     st.s += e;
     st.u = fmaf(e, fmaxf(d, -200.f), st.u); // 0 * -inf would be NaN, and 2^-200 is 0
   };
-  if (fabsf(st.k) < INFINITY) {
+  if (st.k < INFINITY) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) add(fmaf(x[i], c, -st.k));
   } else {
@@ -266,7 +271,7 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
   if constexpr (kWaves > 1) st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, -INFINITY, 0, 0, 0}, c);
   // of base e: lse = top + log_z
   const float top = st.m == -INFINITY ? 0.f : st.m * in.inv_temperature, log2_s = __builtin_amdgcn_logf(st.s);
-  const float past = st.m == -INFINITY || !(fabsf(st.k) < INFINITY) ? 0.f : fmaf(st.m, c, -st.k), log_z = (log2_s - past) * kLn2;
+  const float past = st.m == -INFINITY || !(st.k < INFINITY) ? 0.f : fmaf(st.m, c, -st.k), log_z = (log2_s - past) * kLn2;
   const auto logprob_of = [&](float x) { // nearer than x * inv_temperature - lse, whose terms are rounded where they are large
     return x == -INFINITY && st.s == st.s ? -INFINITY : (x - (st.m == -INFINITY ? 0.f : st.m)) * in.inv_temperature - log_z;
   };
