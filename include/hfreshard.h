@@ -543,6 +543,9 @@ HF_API int hf_append_kv(const hf_kv_cache *cache, const hf_append *args, void *h
  * of the prompt, whose keys and values are read once for all of them.  Then every sequence's own pages (its response, the
  * current token included) follow.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *   x_j = scale * <q, k_j> over all visible tokens j;  out = sum_j exp(x_j - lse) v_j;  lse = log sum_j exp(x_j).
+ * The weights exp(x_j - lse) are held in 32 bits for lse and multiplied as two numbers of the cache's type, upper bits and rest: each is off by at most
+ * 2^-16 of itself (HF_BF16) or of the largest of the 32 tokens that it is taken with (HF_F16; weights below 2^-45 of a row's sum may be left out).
+ * Infinities among the visible keys and values may give NaN.
  * A sequence without any visible token has out = 0 and lse = -inf.  Tokens past a length or on a page number
  * outside the cache are not visible, whatever the cache holds there, NaN included; lengths are cut to the table's
  * width * page_tokens and to max_prefix / max_suffix, below 0 they count as 0.  A sequence in no group has no prompt, and so have the

@@ -22,7 +22,7 @@
 //  - a lane loads 16 bytes of each of its eight tokens' values, whole rows over 16 lanes; the eight rows are turned in its registers (one byte
 //    permute per two elements) into left operands for eight products, product j holding every eighth element of a head.
 // Exponentials are of base 2, the scale carries the factor.  P is rounded to the cache's type twice, once for its upper bits and once for the
-// rest: rounded once it would add as much to the error as the rounding of the output does.
+// rest: rounded once it would add as much to the error as the rounding of the output does.  Twice it is off by 2^-17 of itself in bfloat16; see kUp for float16.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -259,7 +259,15 @@ template <typename T, int kDim, int kMode, bool kLanes, bool kOnce> struct Reade
 
 // 16 rows' softmax so far; m of the products, before the scale.  m follows the largest score only when one is past it by kSlack of base 2 (P is
 // then below 2^kSlack): with 16 rows to a tile some row has a new largest score in nearly every tile, and everything would be rescaled each time.
-constexpr float kSlack = 8;
+// In float16 the two halves of P share the type's smallest step, 2^-24, so that weights far below m would lose their bits one by one, where the tokens above
+// them may have values of 0 (16 nats below: 6 % off; 18: nothing left).  P carries 2^kUp there, which with the slack stays in the type, and where a row's largest
+// score of a tile is kFall below m, m goes down to it: half a step is then 2^-17 of the tile's largest weight at most.  The sums grow by as much, up to
+// 2^kSums: a row's weights of less than 2^-45 of their sum show in no float16 output.
+template <typename T> constexpr bool kNarrow = std::is_same_v<T, _Float16>;
+template <typename T> constexpr float kSlack = kNarrow<T> ? 7 : 8;
+template <typename T> constexpr float kUp = kNarrow<T> ? 8 : 0;
+constexpr float kFall = 16, kSums = 60;
+constexpr float kCoarse = 1 << 22; // scores of base 2 whose own rounding could take P past the type together with the slack
 template <typename T, int kOwn> struct Rows {
   f32x4 o[kOwn];
   float m, l, limit; // limit: m and the slack
@@ -280,16 +288,27 @@ template <typename T, int kOwn> struct Rows {
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-    if (__builtin_amdgcn_ballot_w64(top > limit) != 0) {
-      const float m_new = fmaxf(m, over_rows<Max>(top));
+    bool moves = __builtin_amdgcn_ballot_w64(top > limit) != 0;
+    if constexpr (kNarrow<T>) { // all four lanes of a column
+      uint64_t low = __builtin_amdgcn_ballot_w64(top < limit - (kSlack<T> + kFall) / scale2);
+      low &= low >> 32;
+      moves |= (low & low >> 16 & 0xFFFF) != 0;
+    }
+    if (moves) {
+      top = over_rows<Max>(top);
+      float m_new = fmaxf(m, top);
+      if constexpr (kNarrow<T>) {
+        const float room = kSums - __builtin_amdgcn_logf(over_rows<Sum>(l));
+        if (top < m - kFall / scale2 && top > -INFINITY) m_new = fmaxf(top, m - fmaxf(room, 0.f) / scale2);
+      }
       const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
       m = m_new;
-      limit = m + kSlack / scale2;
+      limit = kNarrow<T> && fabsf(m) * scale2 > kCoarse ? m : m + kSlack<T> / scale2;
       l *= keep;
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) o[j] *= keep;
     }
-    const float base = m == -INFINITY ? 0.f : -m * scale2;
+    const float base = m == -INFINITY ? 0.f : kNarrow<T> ? kUp<T> - m * scale2 : -m * scale2;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale2, base));
     if (!whole) {
@@ -334,8 +353,9 @@ template <int kN, int kMode> __device__ __forceinline__ void write_part(const At
 
 template <typename T, int kN, int kMode>
 __device__ __forceinline__ void write_result(const AttendParams &p, int seq, int head, int part_index, int d0, float top, float scale2, float sum, const float *acc) {
-  if (p.s.direct) write_row<T, kN, kMode>(p, seq, head, d0, top * scale2, sum, acc);
-  else write_part<kN, kMode>(p, ((int64_t)seq * p.a.n_q_heads + head) * (p.s.prefix_parts + p.s.suffix_parts) + part_index, d0, top, top * scale2, sum, acc);
+  const float m2 = kNarrow<T> ? top * scale2 - kUp<T> : top * scale2;
+  if (p.s.direct) write_row<T, kN, kMode>(p, seq, head, d0, m2, sum, acc);
+  else write_part<kN, kMode>(p, ((int64_t)seq * p.a.n_q_heads + head) * (p.s.prefix_parts + p.s.suffix_parts) + part_index, d0, top, m2, sum, acc);
 }
 
 // The parts of a workgroup's wavefronts become one: kRowWaves of them have rows of their own, the others the same rows over other tokens.
