@@ -75,33 +75,28 @@ __device__ __forceinline__ float larger(float a, float b, float c) {
   return r;
 }
 
-// Largest element m, and sums over the elements of 2^d and of 2^d d with d = x c - k, c = log2(e) / temperature.  k is x0 c rounded to a whole number: then d
-// is one operation, with one rounding, and sums move to another k exactly, where x0 c itself would be off by as much as its own rounding.  x0 is
+// Largest element m, and sums over the elements of 2^d and of 2^d d with d = (x - r) c - k, c = log2(e) / temperature.  Up to kWhole r is 0 and k the base x0 c
+// rounded to a whole number: then d is one operation, with one rounding, and sums move to another k exactly, where x0 c itself would be off by as
+// much as its own rounding.  Past it (mask values, low temperatures) that rounding alone would be a whole number and more: there r is x0 and k is 0.  x0 is
 // the largest element of a lane's first vectors and follows m only when that is past it by kSlack of base 2, which for most lanes never happens.
-// Past kWhole (mask values, low temperatures) the product's own rounding would be a whole number and more: k is infinite there, the
-// base x0 itself, and d = (x - x0) c.
 struct Stats {
-  float m, x0, k, s, u;
+  float m, r, k, s, u;
 };
 constexpr float kSlack = 8, kWhole = 1 << 24;
 __device__ __forceinline__ void rebase(Stats &st, float x0, float c) {
-  float k = x0 == -INFINITY ? 0.f : rintf(x0 * c), d = st.k - k;
-  if (!(fmaxf(fabsf(k), st.k) < kWhole)) {
-    const bool was = st.k < INFINITY, is = fabsf(k) < kWhole;
-    d = is ? fmaf(st.x0, c, -k) : was ? -fmaf(x0, c, -st.k) : (st.x0 - x0) * c;
-    if (!is) k = INFINITY;
-  }
-  if (st.x0 == -INFINITY) d = 0; // before the first element there is nothing to move
+  const bool whole = fabsf(x0 * c) < kWhole;
+  const float k = whole ? rintf(x0 * c) : 0.f, r = whole || x0 == -INFINITY ? 0.f : x0;
+  const float d = st.s == 0 ? 0.f : fmaf(st.r - r, c, st.k - k); // (nothing to move before the first element)
   const float down = __builtin_amdgcn_exp2f(d);
   st.u = st.s > 0 ? down * fmaf(fmaxf(d, -200.f), st.s, st.u) : st.u;
   st.s *= down;
-  st.x0 = x0;
+  st.r = r;
   st.k = k;
 }
 __device__ __forceinline__ Stats merge_wave(Stats st, float c) {
   st.m = over_wave<Max>(st.m);
   rebase(st, st.m, c);
-  return {st.m, st.x0, st.k, over_wave<Sum>(st.s), over_wave<Sum>(st.u)};
+  return {st.m, st.r, st.k, over_wave<Sum>(st.s), over_wave<Sum>(st.u)};
 }
 
 // limit: x0 and the slack
@@ -116,12 +111,12 @@ template <int kN> __device__ __forceinline__ void join(Stats &st, float &limit, 
     st.s += e;
     st.u = fmaf(e, fmaxf(d, -200.f), st.u); // 0 * -inf would be NaN, and 2^-200 is 0
   };
-  if (st.k < INFINITY) {
+  if (st.r == 0) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) add(fmaf(x[i], c, -st.k));
   } else {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) add((x[i] - st.x0) * c);
+    for (int i = 0; i < kN; ++i) add((x[i] - st.r) * c);
   }
 }
 
@@ -184,7 +179,7 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
   const float x_target = (float)row[target];
   const float c = in.inv_temperature * kLog2e;
   const int n_vec = vocab / kV; // whole ones
-  Stats st = {-INFINITY, -INFINITY, 0, 0, 0};
+  Stats st = {-INFINITY, 0, 0, 0, 0};
   float limit = -INFINITY;
   float best = -INFINITY;         // the lane's largest element
   uint32_t best_at = 0xFFFFFFFFu; // and the vector that had it first; none: no vectors
@@ -268,10 +263,10 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
   if constexpr (kWaves > 1 || kTop) __syncthreads();
   if constexpr (!kTop)
     if (wave > 0) return; // the rest is a few numbers
-  if constexpr (kWaves > 1) st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, -INFINITY, 0, 0, 0}, c);
+  if constexpr (kWaves > 1) st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, 0, 0, 0, 0}, c);
   // of base e: lse = top + log_z
   const float top = st.m == -INFINITY ? 0.f : st.m * in.inv_temperature, log2_s = __builtin_amdgcn_logf(st.s);
-  const float past = st.m == -INFINITY || !(st.k < INFINITY) ? 0.f : fmaf(st.m, c, -st.k), log_z = (log2_s - past) * kLn2;
+  const float past = st.m == -INFINITY ? 0.f : fmaf(st.m - st.r, c, -st.k), log_z = (log2_s - past) * kLn2;
   const auto logprob_of = [&](float x) { // nearer than x * inv_temperature - lse, whose terms are rounded where they are large
     return x == -INFINITY && st.s == st.s ? -INFINITY : (x - (st.m == -INFINITY ? 0.f : st.m)) * in.inv_temperature - log_z;
   };
