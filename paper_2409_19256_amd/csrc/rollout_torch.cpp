@@ -1,11 +1,12 @@
 // Python module _rollout: the rollout operators' C calls with torch tensors as arguments.  It looks tensors over, makes the outputs that were not
-// given, and fills the argument structs; the smallest calls wait for the host, and in Python this took two to three times as long as the launch (one step
+// given, makes their GPU the current one, and fills the argument structs; the smallest calls wait for the host, and in Python this took two to three times as long as the launch (one step
 // of the tiny decoder's attention 15.8 us a call in Python).  rollout.py documents the functions and is what callers import.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -80,6 +81,11 @@ const hf_kv_cache *cache_of(PyObject *o) {
   if (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof(hf_kv_cache)) throw Wrong{"cache", "an hf_kv_cache in bytes is wanted"};
   return reinterpret_cast<const hf_kv_cache *>(PyBytes_AS_STRING(o));
 }
+// the buffers of a cache, which have to be where the operands are
+void same_gpu(PyObject *keys, PyObject *values, int device) {
+  for (PyObject *o : {keys, values})
+    if (const Tensor &t = wanted(o, "cache"); !t.is_cuda() || t.get_device() != device) throw Wrong{"cache", "a cache on the operands' GPU is wanted"};
+}
 at::ScalarType type_of(const hf_kv_cache &c) { return c.dtype == HF_BF16 ? at::kBFloat16 : at::kHalf; }
 void *stream_of(PyObject *o) {
   void *s = PyLong_AsVoidPtr(o);
@@ -117,15 +123,17 @@ template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, const F &
   END_HANDLE_TH_ERRORS
 }
 
-// (cache, stream, k, v, slots, positions, cos, sin, q, q_out, interleaved) -> q_out
+// (cache, its keys, its values, stream, k, v, slots, positions, cos, sin, q, q_out, interleaved) -> q_out
 PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
-  return guarded(n_args, 11, [&]() -> PyObject * {
+  return guarded(n_args, 13, [&]() -> PyObject * {
     const hf_kv_cache &c = *cache_of(arg[0]);
-    const Tensor &k = wanted(arg[2], "k"), &v = wanted(arg[3], "v"), &slots = wanted(arg[4], "slots");
-    const Tensor *positions = given(arg[5], "positions"), *cos = given(arg[6], "cos"), *sin = given(arg[7], "sin"), *q = given(arg[8], "q");
+    const Tensor &k = wanted(arg[4], "k"), &v = wanted(arg[5], "v"), &slots = wanted(arg[6], "slots");
+    const Tensor *positions = given(arg[7], "positions"), *cos = given(arg[8], "cos"), *sin = given(arg[9], "sin"), *q = given(arg[10], "q");
     const at::ScalarType type = type_of(c);
     if (!k.is_cuda() || k.dim() != 3) throw Wrong{"k", "[token, KV head, element] on the GPU is wanted"};
     const int device = k.get_device();
+    same_gpu(arg[1], arg[2], device);
+    const c10::DeviceGuard current(k.device());
     const int64_t n = k.size(0);
     hf_append a = {};
     const Rows ks = rows_of(k, "k", type, n, c.n_kv_heads, c.head_dim, device), vs = rows_of(v, "v", type, n, c.n_kv_heads, c.head_dim, device);
@@ -148,31 +156,33 @@ PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       const int64_t heads = q->size(1);
       const Rows qs = rows_of(*q, "q", type, n, heads, c.head_dim, device);
       a.q = qs.at, a.q_stride = qs.stride, a.q_head_stride = qs.head_stride, a.n_q_heads = int32_of(heads, "q");
-      const Tensor *out = given(arg[9], "q_out");
+      const Tensor *out = given(arg[11], "q_out");
       if (!out) made = at::empty({n, heads, c.head_dim}, q->options());
       const Rows os = rows_of(out ? *out : made, "q_out", type, n, heads, c.head_dim, device);
       a.q_out = os.at, a.q_out_stride = os.stride, a.q_out_head_stride = os.head_stride;
-      if (out) result = arg[9];
+      if (out) result = arg[11];
     }
-    const int interleaved = PyObject_IsTrue(arg[10]);
+    const int interleaved = PyObject_IsTrue(arg[12]);
     if (interleaved < 0) throw python_error();
     a.flags = interleaved ? HF_ROT_INTERLEAVED : 0;
-    if (const int code = hf_append_kv(&c, &a, stream_of(arg[1]))) return failed(code, "hf_append_kv");
+    if (const int code = hf_append_kv(&c, &a, stream_of(arg[3]))) return failed(code, "hf_append_kv");
     return made.defined() ? wrap(std::move(made)) : again(result ? result : Py_None);
   });
 }
 
-// (cache, stream, q, suffix_lens, suffix_pages, group_offsets, prefix_lens, prefix_pages, max_group, max_prefix, max_suffix, scale, out, lse, workspace)
+// (cache, its keys, its values, stream, q, suffix_lens, suffix_pages, group_offsets, prefix_lens, prefix_pages, max_group, max_prefix, max_suffix, scale, out, lse, workspace)
 // -> (out, lse)
 PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
-  return guarded(n_args, 15, [&]() -> PyObject * {
+  return guarded(n_args, 17, [&]() -> PyObject * {
     const hf_kv_cache &c = *cache_of(arg[0]);
-    const Tensor &q = wanted(arg[2], "q"), &lens = wanted(arg[3], "suffix_lens"), &pages = wanted(arg[4], "suffix_pages");
-    const Tensor *offsets = given(arg[5], "group_offsets"), *prefix_lens = given(arg[6], "prefix_lens"), *prefix_pages = given(arg[7], "prefix_pages");
-    const Tensor *out = given(arg[12], "out"), *lse = given(arg[13], "lse"), *workspace = given(arg[14], "workspace");
+    const Tensor &q = wanted(arg[4], "q"), &lens = wanted(arg[5], "suffix_lens"), &pages = wanted(arg[6], "suffix_pages");
+    const Tensor *offsets = given(arg[7], "group_offsets"), *prefix_lens = given(arg[8], "prefix_lens"), *prefix_pages = given(arg[9], "prefix_pages");
+    const Tensor *out = given(arg[14], "out"), *lse = given(arg[15], "lse"), *workspace = given(arg[16], "workspace");
     const at::ScalarType type = type_of(c);
     if (!q.is_cuda() || q.dim() != 3) throw Wrong{"q", "[sequence, query head, element] on the GPU is wanted"};
     const int device = q.get_device();
+    same_gpu(arg[1], arg[2], device);
+    const c10::DeviceGuard current(q.device());
     const int64_t n = q.size(0), heads = q.size(1);
     hf_attention a = {};
     const Rows qs = rows_of(q, "q", type, n, heads, c.head_dim, device);
@@ -199,10 +209,10 @@ PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       a.prefix_pages = static_cast<const int32_t *>(whole(prefix_pages, "prefix_pages", at::kInt, {groups, prefix_width}, device));
       a.n_groups = int32_of(groups, "prefix_pages"), a.prefix_width = int32_of(prefix_width, "prefix_pages");
     }
-    a.max_group = bound(arg[8], n, "max_group");
-    a.max_prefix = bound(arg[9], std::min<int64_t>(prefix_width * c.page_tokens, INT32_MAX), "max_prefix");
-    a.max_suffix = bound(arg[10], std::min<int64_t>(width * c.page_tokens, INT32_MAX), "max_suffix");
-    a.scale = arg[11] == Py_None ? (float)(1 / std::sqrt((double)c.head_dim)) : (float)real(arg[11]);
+    a.max_group = bound(arg[10], n, "max_group");
+    a.max_prefix = bound(arg[11], std::min<int64_t>(prefix_width * c.page_tokens, INT32_MAX), "max_prefix");
+    a.max_suffix = bound(arg[12], std::min<int64_t>(width * c.page_tokens, INT32_MAX), "max_suffix");
+    a.scale = arg[13] == Py_None ? (float)(1 / std::sqrt((double)c.head_dim)) : (float)real(arg[13]);
     if (workspace) {
       if (!workspace->is_cuda() || workspace->get_device() != device || !workspace->is_contiguous()) throw Wrong{"workspace", "a contiguous tensor on the operands' GPU is wanted"};
       a.workspace = workspace->data_ptr(), a.workspace_bytes = workspace->nbytes();
@@ -214,8 +224,8 @@ PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
         a.workspace = made_workspace.data_ptr(), a.workspace_bytes = size;
       }
     }
-    if (const int code = hf_attend(&c, &a, stream_of(arg[1]))) return failed(code, "hf_attend");
-    PyObject *first = out ? again(arg[12]) : wrap(std::move(made_out)), *second = lse ? again(arg[13]) : wrap(std::move(made_lse));
+    if (const int code = hf_attend(&c, &a, stream_of(arg[3]))) return failed(code, "hf_attend");
+    PyObject *first = out ? again(arg[14]) : wrap(std::move(made_out)), *second = lse ? again(arg[15]) : wrap(std::move(made_lse));
     PyObject *both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
     Py_XDECREF(first);
     Py_XDECREF(second);
@@ -252,6 +262,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
   return guarded(n_args, 5, [&]() -> PyObject * {
     const Tensor &logits = wanted(arg[1], "logits"), *targets = given(arg[2], "targets");
     const hf_logits a = logits_of(logits, targets, arg[3]);
+    const c10::DeviceGuard current(logits.device());
     const int64_t top = number(arg[4]);
     if (top < 0 || top > HF_MAX_TOP) throw Wrong{"top", "0 to HF_MAX_TOP is wanted"};
     const auto options = logits.options().dtype(at::kFloat);
@@ -279,6 +290,7 @@ PyObject *token_logprobs_back(PyObject *, PyObject *const *arg, Py_ssize_t n_arg
   return guarded(n_args, 9, [&]() -> PyObject * {
     const Tensor &logits = wanted(arg[1], "logits"), &targets = wanted(arg[2], "targets"), &norm = wanted(arg[3], "norm");
     const hf_logits a = logits_of(logits, &targets, arg[7]);
+    const c10::DeviceGuard current(logits.device());
     const int device = logits.get_device();
     hf_logprobs_grad g = {};
     g.norm = static_cast<const float *>(whole(&norm, "norm", at::kFloat, {a.rows, 2}, device));

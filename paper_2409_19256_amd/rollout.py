@@ -1,7 +1,7 @@
 """The rollout operators for callers that use PyTorch: a paged cache of keys and values that is appended to and attended
 over, and log probabilities of given tokens with their gradient.  torch allocates and hands out pointers and streams; a
 native module (_rollout) checks types and shapes and calls the library, which checks sizes and strides; all work runs in its HIP kernels
-on torch's current stream.  There is no CPU path.
+on torch's current stream of the tensors' GPU, whichever is current; all tensors of a call are on one.  There is no CPU path.
 """
 from __future__ import annotations
 
@@ -55,7 +55,7 @@ class KvCache:
         negative: left out), the keys turned by cos and sin [position, pairs] at positions[token] (int32); without a table
         they are copied.  q [token, query head, element] is turned the same way into q_out (may be q; made if not given),
         which is returned."""
-        return _native.append(self._c, _stream_of(_device_of(k)), k, v, slots, positions, cos, sin, q, q_out, interleaved)
+        return _native.append(self._c, self.k, self.v, _stream_of(_device_of(k)), k, v, slots, positions, cos, sin, q, q_out, interleaved)
 
     def attend(self, q: torch.Tensor, suffix_lens: torch.Tensor, suffix_pages: torch.Tensor, group_offsets: Optional[torch.Tensor] = None,
                prefix_lens: Optional[torch.Tensor] = None, prefix_pages: Optional[torch.Tensor] = None, max_group: Optional[int] = None,
@@ -65,7 +65,7 @@ class KvCache:
         numbers int32 [sequence, width]) and, where sequences are grouped by prompt, over their prompt's (group_offsets int32
         [prompts + 1], lengths [prompts], page numbers [prompts, width]).  max_*: upper bounds of the samples per
         prompt and of the lengths; by default all sequences and what the tables can name.  Returns (out, lse)."""
-        return _native.attend(self._c, _stream_of(_device_of(q)), q, suffix_lens, suffix_pages, group_offsets, prefix_lens, prefix_pages,
+        return _native.attend(self._c, self.k, self.v, _stream_of(_device_of(q)), q, suffix_lens, suffix_pages, group_offsets, prefix_lens, prefix_pages,
                               max_group, max_prefix, max_suffix, scale, out, lse, workspace)
 
 
