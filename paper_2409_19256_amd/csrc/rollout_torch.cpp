@@ -257,16 +257,16 @@ hf_logits logits_of(const Tensor &logits, const Tensor *targets, PyObject *tempe
   return a;
 }
 
-// (stream, logits, targets, temperature, top) -> (logprob, entropy, lse and norm in one, ids, log probabilities)
+// (stream, logits, targets, temperature, top, apart) -> (logprob, entropy, lse and norm in one, ids, log probabilities, logprob in a tensor of its own if it is wanted apart)
 PyObject *token_logprobs(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
-  return guarded(n_args, 5, [&]() -> PyObject * {
+  return guarded(n_args, 6, [&]() -> PyObject * {
     const Tensor &logits = wanted(arg[1], "logits"), *targets = given(arg[2], "targets");
     const hf_logits a = logits_of(logits, targets, arg[3]);
     const c10::DeviceGuard current(logits.device());
     const int64_t top = number(arg[4]);
     if (top < 0 || top > HF_MAX_TOP) throw Wrong{"top", "0 to HF_MAX_TOP is wanted"};
     const auto options = logits.options().dtype(at::kFloat);
-    Tensor stats = at::empty({5 * a.rows}, options), ids, values;
+    Tensor stats = at::empty({5 * a.rows}, options), ids, values, logprob;
     float *s = static_cast<float *>(stats.data_ptr());
     hf_logprobs o = {};
     o.logprob = targets ? s : nullptr, o.entropy = s + a.rows, o.lse = s + 2 * a.rows, o.norm = s + 3 * a.rows, o.top_n = (int32_t)top;
@@ -275,12 +275,18 @@ PyObject *token_logprobs(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       values = at::empty({a.rows, top}, options);
       o.top_ids = static_cast<int32_t *>(ids.data_ptr()), o.top_logprobs = static_cast<float *>(values.data_ptr());
     }
+    if (targets && arg[5] == Py_True) {
+      logprob = at::empty({a.rows}, options);
+      o.logprob = static_cast<float *>(logprob.data_ptr());
+    }
     if (const int code = hf_token_logprobs(&a, &o, stream_of(arg[0]))) return failed(code, "hf_token_logprobs");
-    PyObject *x = wrap(std::move(stats)), *y = top ? wrap(std::move(ids)) : again(Py_None), *z = top ? wrap(std::move(values)) : again(Py_None);
-    PyObject *all = x && y && z ? PyTuple_Pack(3, x, y, z) : nullptr;
+    const auto made = [](Tensor &t) { return t.defined() ? wrap(std::move(t)) : again(Py_None); };
+    PyObject *x = made(stats), *y = made(ids), *z = made(values), *w = made(logprob);
+    PyObject *all = x && y && z && w ? PyTuple_Pack(4, x, y, z, w) : nullptr;
     Py_XDECREF(x);
     Py_XDECREF(y);
     Py_XDECREF(z);
+    Py_XDECREF(w);
     return all;
   });
 }

@@ -101,7 +101,7 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], temper
     """Log probability of targets[row] (int64 or int32; outside the vocabulary: the row is left out), entropy, log sum of exponentials
     (lse, and in two parts for token_logprobs_back: norm) and the `top` likeliest tokens of every row of logits [rows, vocab] over the
     temperature.  Not differentiable by itself: see logprobs."""
-    stats, ids, values = _native.token_logprobs(_stream_of(_device_of(logits)), logits, targets, temperature, top)
+    stats, ids, values, _ = _native.token_logprobs(_stream_of(_device_of(logits)), logits, targets, temperature, top, False)
     return Logprobs(stats, len(logits), targets is not None, ids, values)
 
 
@@ -115,10 +115,11 @@ def token_logprobs_back(logits: torch.Tensor, targets: torch.Tensor, norm: torch
 class _Logprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, temperature):
-        r = token_logprobs(logits, targets, temperature)
+        stats, _, _, logprob = _native.token_logprobs(_stream_of(_device_of(logits)), logits, targets, temperature, 0, True)
+        r = Logprobs(stats, len(logits), True, None, None)
         ctx.save_for_backward(logits, targets, r.norm, r.entropy)
         ctx.temperature = temperature
-        return r.logprob, r.entropy
+        return logprob, r.entropy.clone()  # the caller's own, both: a loss may mask them in place
 
     @staticmethod
     @torch.autograd.function.once_differentiable
