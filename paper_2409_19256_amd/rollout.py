@@ -131,4 +131,5 @@ class _Logprobs(torch.autograd.Function):
 
 def logprobs(logits: torch.Tensor, targets: torch.Tensor, temperature: float = 1.0):
     """(log probability of targets, entropy) of every row, differentiable with respect to the logits."""
+    _need(targets is not None, "targets: a tensor is wanted (entropy alone: token_logprobs)")
     return _Logprobs.apply(logits, targets, temperature)
