@@ -7,6 +7,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -86,6 +87,12 @@ void same_gpu(PyObject *keys, PyObject *values, int device) {
   for (PyObject *o : {keys, values})
     if (const Tensor &t = wanted(o, "cache"); !t.is_cuda() || t.get_device() != device) throw Wrong{"cache", "a cache on the operands' GPU is wanted"};
 }
+// The cache's operators have no backward: where torch would take a gradient they refuse, rather than lose it in silence.
+void without_gradient(std::initializer_list<std::pair<const char *, const Tensor *>> tensors) {
+  if (!c10::GradMode::is_enabled()) return;
+  for (const auto &[name, t] : tensors)
+    if (t && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
+}
 at::ScalarType type_of(const hf_kv_cache &c) { return c.dtype == HF_BF16 ? at::kBFloat16 : at::kHalf; }
 void *stream_of(PyObject *o) {
   void *s = PyLong_AsVoidPtr(o);
@@ -149,6 +156,8 @@ PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       a.positions = static_cast<const int32_t *>(whole(positions, "positions", at::kInt, {n}, device));
       a.rot_dim = int32_of(2 * pairs, "cos"), a.n_positions = int32_of(table, "cos");
     }
+    const Tensor *out = q ? given(arg[11], "q_out") : nullptr;
+    without_gradient({{"cache", &wanted(arg[1], "cache")}, {"cache", &wanted(arg[2], "cache")}, {"k", &k}, {"v", &v}, {"q", q}, {"q_out", out}});
     PyObject *result = nullptr;
     Tensor made;
     if (q) {
@@ -156,7 +165,6 @@ PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       const int64_t heads = q->size(1);
       const Rows qs = rows_of(*q, "q", type, n, heads, c.head_dim, device);
       a.q = qs.at, a.q_stride = qs.stride, a.q_head_stride = qs.head_stride, a.n_q_heads = int32_of(heads, "q");
-      const Tensor *out = given(arg[11], "q_out");
       if (!out) made = at::empty({n, heads, c.head_dim}, q->options());
       const Rows os = rows_of(out ? *out : made, "q_out", type, n, heads, c.head_dim, device);
       a.q_out = os.at, a.q_out_stride = os.stride, a.q_out_head_stride = os.head_stride;
@@ -183,6 +191,7 @@ PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     const int device = q.get_device();
     same_gpu(arg[1], arg[2], device);
     const c10::DeviceGuard current(q.device());
+    without_gradient({{"cache", &wanted(arg[1], "cache")}, {"cache", &wanted(arg[2], "cache")}, {"q", &q}, {"out", out}, {"lse", lse}});
     const int64_t n = q.size(0), heads = q.size(1);
     hf_attention a = {};
     const Rows qs = rows_of(q, "q", type, n, heads, c.head_dim, device);

@@ -33,7 +33,8 @@ def _device_of(t) -> int:
 
 class KvCache:
     """Keys and values, each [page, KV head, token of the page, element] in any order of memory with the last contiguous
-    (`KvCache.empty` makes one), for hf_append_kv and hf_attend."""
+    (`KvCache.empty` makes one), for hf_append_kv and hf_attend.  Both are for generation and scoring: they take no gradient, and refuse
+    tensors that require one where torch would take it (call them under torch.no_grad())."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.is_cuda and k.device == v.device,
