@@ -93,6 +93,11 @@ void without_gradient(std::initializer_list<std::pair<const char *, const Tensor
   for (const auto &[name, t] : tensors)
     if (t && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
 }
+// what a call has written to, for whoever saved it for a backward pass
+void written(std::initializer_list<const Tensor *> tensors) {
+  for (const Tensor *t : tensors)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 at::ScalarType type_of(const hf_kv_cache &c) { return c.dtype == HF_BF16 ? at::kBFloat16 : at::kHalf; }
 void *stream_of(PyObject *o) {
   void *s = PyLong_AsVoidPtr(o);
@@ -174,6 +179,7 @@ PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     if (interleaved < 0) throw python_error();
     a.flags = interleaved ? HF_ROT_INTERLEAVED : 0;
     if (const int code = hf_append_kv(&c, &a, stream_of(arg[3]))) return failed(code, "hf_append_kv");
+    written({&wanted(arg[1], "cache"), &wanted(arg[2], "cache"), out});
     return made.defined() ? wrap(std::move(made)) : again(result ? result : Py_None);
   });
 }
@@ -234,6 +240,7 @@ PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
       }
     }
     if (const int code = hf_attend(&c, &a, stream_of(arg[3]))) return failed(code, "hf_attend");
+    written({out, lse, workspace});
     PyObject *first = out ? again(arg[14]) : wrap(std::move(made_out)), *second = lse ? again(arg[15]) : wrap(std::move(made_lse));
     PyObject *both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
     Py_XDECREF(first);
@@ -320,6 +327,7 @@ PyObject *token_logprobs_back(PyObject *, PyObject *const *arg, Py_ssize_t n_arg
     if (to.stride(1) != 1 && to.size(1) != 1) throw Wrong{"out", "the last dimension has to be contiguous"};
     g.dlogits = to.data_ptr(), g.dlogits_stride = to.stride(0);
     if (const int code = hf_token_logprobs_back(&a, &g, stream_of(arg[0]))) return failed(code, "hf_token_logprobs_back");
+    written({out});
     return out ? again(arg[8]) : wrap(std::move(made));
   });
 }

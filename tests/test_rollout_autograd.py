@@ -61,3 +61,46 @@ def run(script, module, last):
 def test_a_gradient_is_not_lost_in_silence(module):  # noqa: F811
     """The cache's operators have no backward: asked for one, they refuse."""
     run(GRADIENTS, module, "gradients ok")
+
+
+VERSIONS = """
+import sys
+import torch
+from tests.rollout_module import Stand
+s = Stand(sys.argv[1])
+R, i32, f32 = s.rollout, torch.int32, torch.float32
+
+
+def written(tensors, run):
+    before = {n: t._version for n, t in tensors.items()}
+    run()
+    return sorted(n for n, t in tensors.items() if t._version != before[n])
+
+
+c = R.KvCache(s.tensor(3, 2, 4, 8), s.tensor(3, 2, 4, 8))
+slots, lens, pages = s.tensor(5, dtype=torch.int64), s.tensor(6, dtype=i32), s.tensor(6, 2, dtype=i32)
+t = dict(cache_k=c.k, cache_v=c.v, k=s.tensor(5, 2, 8), v=s.tensor(5, 2, 8), q=s.tensor(5, 4, 8), q_out=s.tensor(5, 4, 8))
+append = lambda k=t["k"], v=t["v"], **kw: c.append(k, v, slots, **kw)
+assert written(t, append) == ["cache_k", "cache_v"]
+assert written(t, lambda: append(q=t["q"])) == ["cache_k", "cache_v"]
+assert written(t, lambda: append(q=t["q"], q_out=t["q_out"])) == ["cache_k", "cache_v", "q_out"]
+assert written(t, lambda: append(q=t["q"], q_out=t["q"])) == ["cache_k", "cache_v", "q"]
+t = dict(cache_k=c.k, cache_v=c.v, q=s.tensor(6, 4, 8), out=s.tensor(6, 4, 8), lse=s.tensor(6, 4, dtype=f32), workspace=s.tensor(4096, dtype=f32))
+assert written(t, lambda: c.attend(t["q"], lens, pages)) == []
+assert written(t, lambda: c.attend(t["q"], lens, pages, out=t["out"], lse=t["lse"], workspace=t["workspace"])) == ["lse", "out", "workspace"]
+t = dict(logits=s.tensor(3, 50), out=s.tensor(3, 50), targets=s.tensor(3, dtype=torch.int64), norm=s.tensor(3, 2, dtype=f32), g=s.tensor(3, dtype=f32))
+back = lambda **kw: R.token_logprobs_back(t["logits"], t["targets"], t["norm"], t["g"], t["g"], t["g"], **kw)
+assert written(t, back) == []
+assert written(t, lambda: back(out=t["out"])) == ["out"]
+assert written(t, lambda: back(out=t["logits"])) == ["logits"]
+with torch.inference_mode():  # tensors made here have no version
+    c = R.KvCache(s.tensor(3, 2, 4, 8).view(3, 2, 4, 8), s.tensor(3, 2, 4, 8).view(3, 2, 4, 8))
+    append()
+append()
+print("versions ok")
+"""
+
+
+def test_torch_knows_what_is_written_to(module):  # noqa: F811
+    """A later backward over an overwritten tensor is caught by its version."""
+    run(VERSIONS, module, "versions ok")
