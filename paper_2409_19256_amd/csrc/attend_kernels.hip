@@ -673,8 +673,7 @@ template <typename T, int kDim> __global__ __launch_bounds__(kThreads) void atte
   if (a.lse && lane == 0) a.lse[row] = sum == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, hipStream_t st) {
-  const AttendShape &s = p.s;
+template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(const AttendParams &p, const AttendLaunch &s, hipStream_t st) {
   if (s.small) return enqueue_kernel(attend_small<T, kDim, kMode, kLanes>, dim3((uint32_t)s.suffix_wgs), kThreads, st, p);
   uint32_t prefix_wgs = (uint32_t)s.prefix_wgs, suffix_wgs = (uint32_t)s.suffix_wgs;
   hipError_t e = hipSuccess;
@@ -695,30 +694,25 @@ template <typename T, int kDim, int kMode, bool kLanes> hipError_t launch_mode(c
     e = enqueue_kernel(attend_parts<T, kDim, 4, 1, 1, kMode, kLanes, true>, dim3(prefix_wgs + suffix_wgs), 4 * kWave, st, p, prefix_wgs);
   }
   if (e != hipSuccess || s.direct) return e;
-  const int64_t rows = (int64_t)p.a.n_seqs * p.a.n_q_heads;
-  constexpr int kTeams = kThreads / (kDim / 4);
-  int split = 1;
-  while (split < kTeams && 4 * split < s.prefix_parts + s.suffix_parts) split *= 2;
-  const int rows_of_wg = kTeams / split;
-  return enqueue_kernel(attend_merge<T, kDim>, dim3((uint32_t)((rows + rows_of_wg - 1) / rows_of_wg)), kThreads, st, p, split);
+  return enqueue_kernel(attend_merge<T, kDim>, dim3((uint32_t)s.merge_wgs), kThreads, st, p, s.merge_split);
 }
-template <typename T, int kDim> hipError_t launch_dim(const AttendParams &p, bool vec, hipStream_t st) {
-  if (!vec) return launch_mode<T, kDim, kElements, true>(p, st);
-  if (p.head_dim != kDim) return launch_mode<T, kDim, kPieces, true>(p, st);
-  return p.s.lanes ? launch_mode<T, kDim, kWhole, true>(p, st) : launch_mode<T, kDim, kWhole, false>(p, st);
+template <typename T, int kDim> hipError_t launch_dim(const AttendParams &p, const AttendLaunch &s, bool vec, hipStream_t st) {
+  if (!vec) return launch_mode<T, kDim, kElements, true>(p, s, st);
+  if (p.head_dim != kDim) return launch_mode<T, kDim, kPieces, true>(p, s, st);
+  return s.lanes ? launch_mode<T, kDim, kWhole, true>(p, s, st) : launch_mode<T, kDim, kWhole, false>(p, s, st);
 }
-template <typename T> hipError_t launch_type(const AttendParams &p, bool vec, hipStream_t st) {
-  if (p.head_dim <= 64) return launch_dim<T, 64>(p, vec, st);
-  if (p.head_dim <= 128) return launch_dim<T, 128>(p, vec, st);
-  return launch_dim<T, 256>(p, vec, st);
+template <typename T> hipError_t launch_type(const AttendParams &p, const AttendLaunch &s, bool vec, hipStream_t st) {
+  if (p.head_dim <= 64) return launch_dim<T, 64>(p, s, vec, st);
+  if (p.head_dim <= 128) return launch_dim<T, 128>(p, s, vec, st);
+  return launch_dim<T, 256>(p, s, vec, st);
 }
 
 } // namespace
 
 constexpr uint64_t kResident = 3 * 256; // workgroups of four wavefronts that the chip holds
 
-AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool vec) {
-  AttendShape s = {};
+AttendLaunch attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool vec) {
+  AttendLaunch s = {};
   const int64_t page = cache.page_tokens, ratio = a.n_q_heads / cache.n_kv_heads;
   s.max_suffix = (int32_t)std::min<int64_t>(a.max_suffix, std::min<int64_t>(a.suffix_width * page, 1 << 30));
   s.max_prefix = a.n_groups ? (int32_t)std::min<int64_t>(a.max_prefix, std::min<int64_t>(a.prefix_width * page, 1 << 30)) : 0;
@@ -772,11 +766,20 @@ AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool v
   const int64_t tokens = (int64_t)s.max_prefix + s.max_suffix, one = (int64_t)a.n_seqs * s.suffix_blocks * cache.n_kv_heads;
   const int64_t padded = cache.head_dim <= 64 ? 64 : cache.head_dim <= 128 ? 128 : 256;
   s.small = !s.direct && tokens <= (vec ? (one < 128 ? 640 : 1024) * 128 / padded : 128) && one * tokens <= 1 << 19;
-  if (s.small) s.direct = true, s.prefix_wgs = 0, s.suffix_wgs = one;
+  if (s.small) s.direct = true, s.prefix_wgs = 0, s.suffix_wgs = one, s.row_waves = 0, s.brief = s.together = false;
+  s.merge_split = 1;
+  const int64_t teams = kThreads / (padded / 4);
+  while (s.merge_split < teams && 4 * s.merge_split < s.prefix_parts + s.suffix_parts) s.merge_split *= 2;
+  const int64_t rows_of_merge = teams / s.merge_split;
+  s.merge_wgs = s.direct ? 0 : ((int64_t)a.n_seqs * a.n_q_heads + rows_of_merge - 1) / rows_of_merge;
+  // what launch_mode starts
+  const uint64_t shared = s.row_waves ? s.prefix_wgs + (s.together ? s.suffix_wgs : 0) : 0;
+  const uint64_t parts = s.together ? 0 : (s.row_waves ? 0 : s.prefix_wgs) + (s.brief ? 0 : s.suffix_wgs), brief = s.brief ? (s.suffix_wgs + 3) / 4 : 0;
+  s.fits = shared <= kMaxWgs / 2 && parts <= kMaxWgs && brief <= kMaxWgs && s.merge_wgs <= kMaxWgs;
   return s;
 }
 
-int launch_attend(const hf_kv_cache &cache, const hf_attention &a, const AttendShape &s, bool vec, void *stream) {
+int launch_attend(const hf_kv_cache &cache, const hf_attention &a, const AttendLaunch &s, bool vec, void *stream) {
   AttendParams p = {a, s, static_cast<const char *>(cache.k), static_cast<const char *>(cache.v), 2 * cache.page_stride, 2 * cache.head_stride,
                     2 * cache.token_stride, (uint32_t)cache.n_pages,
                     cache.n_kv_heads, cache.head_dim, __builtin_ctz(cache.page_tokens), a.n_q_heads / cache.n_kv_heads, a.scale * kLog2e, nullptr, nullptr};
@@ -785,7 +788,7 @@ int launch_attend(const hf_kv_cache &cache, const hf_attention &a, const AttendS
     p.part_ml = p.part_o + (size_t)a.n_seqs * a.n_q_heads * (s.prefix_parts + s.suffix_parts) * cache.head_dim;
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return (int)(cache.dtype == HF_BF16 ? launch_type<__bf16>(p, vec, st) : launch_type<_Float16>(p, vec, st));
+  return (int)(cache.dtype == HF_BF16 ? launch_type<__bf16>(p, s, vec, st) : launch_type<_Float16>(p, s, vec, st));
 }
 
 } // namespace hf

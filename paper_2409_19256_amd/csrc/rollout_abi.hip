@@ -182,8 +182,8 @@ int hf_attend(const hf_kv_cache *cache, const hf_attention *args, void *hip_stre
   if (!separate(out, c.head_dim)) return set_error(HF_EINVAL, "the output overlaps itself");
   if (overlap(a.q, 2 * in, a.out, 2 * to)) return set_error(HF_EINVAL, "the output overlaps the queries");
   const bool vec = attention_vec(c, a);
-  const hf::AttendShape shape = hf::attend_shape(c, a, vec);
-  if (shape.prefix_wgs + shape.suffix_wgs > hf::kMaxWgs) return set_error(HF_ERANGE, "too much work for one launch");
+  const hf::AttendLaunch shape = hf::attend_shape(c, a, vec);
+  if (!shape.fits) return set_error(HF_ERANGE, "too much work for one launch");
   if (shape.workspace) {
     if (!a.workspace || !aligned(a.workspace, 16)) return set_error(HF_EINVAL, "the workspace must be given and 16-byte aligned");
     if (a.workspace_bytes < shape.workspace) return set_error(HF_EINVAL, "the workspace is smaller than hf_attend_workspace_bytes says");

@@ -41,10 +41,16 @@ struct AttendShape {
   uint64_t prefix_wgs, suffix_wgs;
   size_t workspace;
 };
+// and what only the host needs of it
+struct AttendLaunch : AttendShape {
+  int32_t merge_split; // teams of lanes that share a row's parts in the merge
+  uint64_t merge_wgs;
+  bool fits; // every launch into a grid of fewer than 2^32 threads
+};
 // vec: every address, stride and the head are multiples of 8 elements
-AttendShape attend_shape(const hf_kv_cache &cache, const hf_attention &args, bool vec);
+AttendLaunch attend_shape(const hf_kv_cache &cache, const hf_attention &args, bool vec);
 // vec: every address, stride and the head are multiples of 8 elements
-int launch_attend(const hf_kv_cache &cache, const hf_attention &args, const AttendShape &shape, bool vec, void *stream);
+int launch_attend(const hf_kv_cache &cache, const hf_attention &args, const AttendLaunch &shape, bool vec, void *stream);
 
 int launch_token_logprobs(const hf_logits &in, const hf_logprobs &out, void *stream);
 int launch_token_logprobs_back(const hf_logits &in, const hf_logprobs_grad &grad, void *stream);
