@@ -500,7 +500,8 @@ HF_API int hf_plan_validate(const hf_plan *plan);
  * entry outside its range is left out as said below and never leads to an access outside the buffers.  Sums, softmax
  * statistics and rotations are held in 32 bits and rounded once to the type of the output.  Results do not depend
  * on what else runs: nothing is added up by atomics.  HF_EINVAL: null pointer, unknown type or flag, size or stride out of contract,
- * output that overlaps itself or an input; HF_ERANGE: a call that does not fit one HIP grid. */
+ * output that overlaps itself, an input or another output (of tensors that lie between one another's rows this is known where their strides
+ * are alike; others are refused); HF_ERANGE: a call that does not fit one HIP grid. */
 enum { HF_BF16 = 0, HF_F16 = 1, HF_F32 = 2 }; /* element types */
 
 /* A paged cache of keys and values.  Element (page, head, token, i) of either is at

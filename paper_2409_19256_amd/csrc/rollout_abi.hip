@@ -1,7 +1,9 @@
 // C entry points of the rollout operators (declarations and contracts: include/hfreshard.h): the checks of what they are given.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "hfreshard.h"
 #include "kernels.hpp"
@@ -51,9 +53,76 @@ template <size_t kN> bool separate(const Dim (&dims)[kN], int64_t inner) {
   return true;
 }
 
-bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uint64_t)b_bytes && y < x + (uint64_t)a_bytes;
+// Where a tensor lies, in bytes: `inner` of them in a row at every step of the dimensions, all from `begin` to `end` (both 0: nowhere).
+struct Place {
+  uintptr_t begin = 0, end = 0;
+  int64_t inner = 0;
+  Dim dims[3] = {{1, 0}, {1, 0}, {1, 0}};
+};
+Place array(const void *at, int64_t n, int64_t size) {
+  Place p;
+  if (!at || n <= 0) return p;
+  p.inner = n > (INT64_MAX >> 3) / size ? INT64_MAX >> 3 : n * size;
+  p.begin = reinterpret_cast<uintptr_t>(at), p.end = p.begin + p.inner;
+  return p;
+}
+// of a tensor whose span() is known to be in contract
+template <size_t kN> Place place(const void *at, const Dim (&dims)[kN], int64_t inner, int64_t size) {
+  Place p = array(at, inner, size);
+  for (size_t i = 0; i < kN; ++i) {
+    if (dims[i].n == 0) return Place{};
+    p.dims[i] = {dims[i].n, dims[i].stride * size};
+    p.end += (dims[i].n - 1) * p.dims[i].stride;
+  }
+  return at ? p : Place{};
+}
+
+// Whether the runs of bytes that begin `apart` from one another and at any whole numbers of steps more meet; steps are by descending stride.
+bool meet_steps(__int128 apart, int64_t a_inner, int64_t b_inner, const Dim *steps, const int64_t (&a_n)[3], const int64_t (&b_n)[3], int i) {
+  while (i < 3 && a_n[i] <= 1 && b_n[i] <= 1) ++i;
+  if (i == 3) return -b_inner < apart && apart < a_inner;
+  const int64_t stride = steps[i].stride;
+  __int128 j = -apart / stride; // what is below reaches no further than a step: at most the three nearest ones bring them together
+  for (__int128 k = j - 1; k <= j + 1; ++k)
+    if (k >= -(a_n[i] - 1) && k <= b_n[i] - 1 && meet_steps(apart + k * stride, a_inner, b_inner, steps, a_n, b_n, i + 1)) return true;
+  return false;
+}
+
+// Whether two tensors share a byte.  Exact where neither reaches into the other's range, and where their strides are alike (slices of one tensor, such as
+// the queries and keys of one projection); otherwise tensors whose ranges meet are taken to.
+bool overlap(const Place &a, const Place &b) { // (an empty place is before all others)
+  if (a.begin >= b.end || b.begin >= a.end) return false;
+  Dim steps[3] = {};
+  int64_t a_n[3], b_n[3];
+  for (int i = 0; i < 3; ++i) {
+    const Dim &d = a.dims[i], &e = b.dims[i];
+    if (d.n > 1 && e.n > 1 && d.stride != e.stride) return true;
+    steps[i] = {i, d.n > 1 ? d.stride : e.n > 1 ? e.stride : 0};
+  }
+  std::sort(steps, steps + 3, [](const Dim &d, const Dim &e) { return d.stride > e.stride; });
+  for (int i = 0; i < 3; ++i) a_n[i] = a.dims[steps[i].n].n, b_n[i] = b.dims[steps[i].n].n;
+  int64_t reach = std::max(a.inner, b.inner); // nested: what lies below a step is within it
+  for (int i = 2; i >= 0; --i) {
+    const int64_t n = std::max(a_n[i], b_n[i]);
+    if (n <= 1) continue;
+    if (steps[i].stride < reach) return true;
+    reach += (n - 1) * steps[i].stride;
+  }
+  return meet_steps((__int128)b.begin - (__int128)a.begin, a.inner, b.inner, steps, a_n, b_n, 0);
+}
+// the first of the outputs that lies in an input or in another output, by its name; null: none
+struct Output {
+  const char *what;
+  Place place;
+};
+template <size_t kN> const char *first_overlap(const Output (&outputs)[kN], std::initializer_list<Place> inputs) {
+  for (size_t i = 0; i < kN; ++i) {
+    for (const Place &p : inputs)
+      if (overlap(outputs[i].place, p)) return outputs[i].what;
+    for (size_t j = 0; j < i; ++j)
+      if (overlap(outputs[i].place, outputs[j].place)) return outputs[i].what;
+  }
+  return nullptr;
 }
 
 // whether a tensor's vectors of `vec` 2-byte elements are aligned wherever they begin
@@ -144,11 +213,20 @@ int hf_append_kv(const hf_kv_cache *cache, const hf_append *args, void *hip_stre
   const Dim page[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
   if (!span(k, c.head_dim) || !span(v, c.head_dim)) return set_error(HF_EINVAL, "strides of keys or values are negative or span too much");
   if (a.q) {
-    const int64_t in = span(q, c.head_dim), out = span(q_out, c.head_dim);
-    if (!in || !out) return set_error(HF_EINVAL, "strides of queries are negative or span too much");
+    if (!span(q, c.head_dim) || !span(q_out, c.head_dim)) return set_error(HF_EINVAL, "strides of queries are negative or span too much");
     if (!separate(q_out, c.head_dim)) return set_error(HF_EINVAL, "q_out overlaps itself");
+  }
+  {
     const bool same = a.q == a.q_out && (a.n_tokens == 1 || a.q_stride == a.q_out_stride) && (a.n_q_heads == 1 || a.q_head_stride == a.q_out_head_stride);
-    if (!same && overlap(a.q, 2 * in, a.q_out, 2 * out)) return set_error(HF_EINVAL, "q_out overlaps q and is not q");
+    const Place from = a.q ? place(a.q, q, c.head_dim, 2) : Place{}, to = a.q ? place(a.q_out, q_out, c.head_dim, 2) : Place{};
+    if (!same && overlap(from, to)) return set_error(HF_EINVAL, "q_out overlaps q and is not q");
+    const int64_t table = a.rot_dim ? (int64_t)a.n_positions * (a.rot_dim / 2) : 0;
+    const Output outputs[] = {{"keys of the cache overlap an input", place(c.k, page, c.head_dim, 2)},
+                              {"values of the cache overlap an input or its keys", place(c.v, page, c.head_dim, 2)},
+                              {"q_out overlaps an input or the cache", to}};
+    if (const char *what = first_overlap(outputs, {place(a.k, k, c.head_dim, 2), place(a.v, v, c.head_dim, 2), same ? Place{} : from, array(a.cos, table, 4),
+                                                   array(a.sin, table, 4), array(a.positions, a.rot_dim ? a.n_tokens : 0, 4), array(a.slots, a.n_tokens, 8)}))
+      return set_error(HF_EINVAL, what);
   }
   if ((uint64_t)a.n_tokens > hf::kMaxWgs) return set_error(HF_ERANGE, "too many tokens for one launch");
   int vec = 8;
@@ -177,10 +255,8 @@ int hf_attend(const hf_kv_cache *cache, const hf_attention *args, void *hip_stre
       !aligned(a.group_offsets, 4) || !aligned(a.prefix_lens, 4) || !aligned(a.prefix_pages, 4))
     return set_error(HF_EINVAL, "arrays must be aligned to their elements");
   const Dim q[] = {{a.n_seqs, a.q_stride}, {a.n_q_heads, a.q_head_stride}}, out[] = {{a.n_seqs, a.out_stride}, {a.n_q_heads, a.out_head_stride}};
-  const int64_t in = span(q, c.head_dim), to = span(out, c.head_dim);
-  if (!in || !to) return set_error(HF_EINVAL, "strides of queries or output are negative or span too much");
+  if (!span(q, c.head_dim) || !span(out, c.head_dim)) return set_error(HF_EINVAL, "strides of queries or output are negative or span too much");
   if (!separate(out, c.head_dim)) return set_error(HF_EINVAL, "the output overlaps itself");
-  if (overlap(a.q, 2 * in, a.out, 2 * to)) return set_error(HF_EINVAL, "the output overlaps the queries");
   const bool vec = attention_vec(c, a);
   const hf::AttendLaunch shape = hf::attend_shape(c, a, vec);
   if (!shape.fits) return set_error(HF_ERANGE, "too much work for one launch");
@@ -188,6 +264,15 @@ int hf_attend(const hf_kv_cache *cache, const hf_attention *args, void *hip_stre
     if (!a.workspace || !aligned(a.workspace, 16)) return set_error(HF_EINVAL, "the workspace must be given and 16-byte aligned");
     if (a.workspace_bytes < shape.workspace) return set_error(HF_EINVAL, "the workspace is smaller than hf_attend_workspace_bytes says");
   }
+  const Dim page[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
+  const int64_t n = a.n_seqs, groups = a.n_groups;
+  const Output outputs[] = {{"the output overlaps an input", place(a.out, out, c.head_dim, 2)},
+                            {"lse overlaps an input or the output", array(a.lse, n * a.n_q_heads, 4)},
+                            {"the workspace overlaps an input or an output", array(a.workspace, shape.direct ? 0 : (int64_t)shape.workspace, 1)}};
+  if (const char *what = first_overlap(outputs, {place(a.q, q, c.head_dim, 2), place(c.k, page, c.head_dim, 2), place(c.v, page, c.head_dim, 2), array(a.suffix_lens, n, 4),
+                                                 array(a.suffix_pages, n * a.suffix_width, 4), array(a.group_offsets, groups ? groups + 1 : 0, 4),
+                                                 array(a.prefix_lens, groups, 4), array(a.prefix_pages, groups * a.prefix_width, 4)}))
+    return set_error(HF_EINVAL, what);
   return launched(hf::launch_attend(c, a, shape, vec, hip_stream));
 }
 
@@ -200,6 +285,15 @@ int hf_token_logprobs(const hf_logits *in, const hf_logprobs *out, void *hip_str
     return set_error(HF_EINVAL, "arrays must be aligned to their elements");
   if (in->rows == 0) return HF_OK;
   if ((uint64_t)in->rows > hf::kMaxWgs / 4) return set_error(HF_ERANGE, "too many rows for one launch"); // workgroups of up to 1024 lanes
+  const Dim from[] = {{in->rows, in->row_stride}};
+  const Output outputs[] = {{"logprob overlaps an input", array(out->logprob, in->rows, 4)},
+                            {"entropy overlaps an input or another output", array(out->entropy, in->rows, 4)},
+                            {"lse overlaps an input or another output", array(out->lse, in->rows, 4)},
+                            {"norm overlaps an input or another output", array(out->norm, 2 * in->rows, 4)},
+                            {"top_ids overlap an input or another output", array(out->top_ids, in->rows * out->top_n, 4)},
+                            {"top_logprobs overlap an input or another output", array(out->top_logprobs, in->rows * out->top_n, 4)}};
+  if (const char *what = first_overlap(outputs, {place(in->logits, from, in->vocab, in->dtype == HF_F32 ? 4 : 2), array(in->targets, in->rows, in->target_bytes)}))
+    return set_error(HF_EINVAL, what);
   return launched(hf::launch_token_logprobs(*in, *out, hip_stream));
 }
 
@@ -213,14 +307,17 @@ int hf_token_logprobs_back(const hf_logits *in, const hf_logprobs_grad *grad, vo
   if (!aligned(grad->norm, 4) || !aligned(grad->entropy, 4) || !aligned(grad->grad_logprob, 4) || !aligned(grad->grad_entropy, 4) || !aligned(grad->dlogits, size))
     return set_error(HF_EINVAL, "arrays must be aligned to their elements");
   const Dim from[] = {{in->rows, in->row_stride}}, to[] = {{in->rows, grad->dlogits_stride}};
-  const int64_t out = span(to, in->vocab);
-  if (!out) return set_error(HF_EINVAL, "dlogits_stride is negative or spans too much");
+  if (!span(to, in->vocab)) return set_error(HF_EINVAL, "dlogits_stride is negative or spans too much");
   if (!separate(to, in->vocab)) return set_error(HF_EINVAL, "dlogits overlaps itself");
-  const bool same = in->logits == grad->dlogits && (in->rows == 1 || in->row_stride == grad->dlogits_stride);
-  if (!same && overlap(in->logits, size * span(from, in->vocab), grad->dlogits, size * out))
-    return set_error(HF_EINVAL, "dlogits overlaps the logits and is not the logits");
   if ((uint64_t)in->rows > hf::kMaxWgs || (uint64_t)in->rows * hf::logprob_back_segments(*in) > hf::kMaxWgs)
     return set_error(HF_ERANGE, "too many rows for one launch");
+  const bool same = in->logits == grad->dlogits && (in->rows == 1 || in->row_stride == grad->dlogits_stride);
+  const Place logits = place(in->logits, from, in->vocab, size);
+  const Output outputs[] = {{"dlogits overlaps an input and is not the logits", place(grad->dlogits, to, in->vocab, size)}};
+  if (const char *what = first_overlap(outputs, {same ? Place{} : logits, array(in->targets, in->rows, in->target_bytes), array(grad->norm, 2 * in->rows, 4),
+                                                 array(grad->grad_entropy ? grad->entropy : nullptr, in->rows, 4), array(grad->grad_logprob, in->rows, 4),
+                                                 array(grad->grad_entropy, in->rows, 4)}))
+    return set_error(HF_EINVAL, what);
   return launched(hf::launch_token_logprobs_back(*in, *grad, hip_stream));
 }
 
