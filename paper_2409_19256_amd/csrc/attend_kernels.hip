@@ -12,9 +12,9 @@
 //  - a wavefront takes tiles of 32 tokens straight from memory into registers, keys and values of the next tile on their way while it works on
 //    the present one; nothing is staged and no wavefront waits for another until its part is done.  Where a prompt has many
 //    rows, eight wavefronts of a workgroup share its tokens and rows, so that a SIMD has two (prompts brought into LDS by the whole workgroup were
-//    no faster: 54 us where this takes 51, 61 samples of 32749 tokens with 488 rows; a SIMD issues vector instructions 29 % of that time, its matrix unit
+//    no faster: 54 us where this takes 51, 61 samples of 32749 tokens with 488 rows; a SIMD issues vector instructions 30 % of that time, its matrix unit
 //    is busy 19 %, and two wavefronts hide no more of each other's waits);
-//  - what is read for one workgroup alone goes past the caches (responses of the 7B shape, 1024 tokens each: 6.8 TB/s, plain loads 6.0);
+//  - what is read for one workgroup alone goes past the caches (responses of the 7B shape, 1024 tokens each: 6.7 TB/s, plain loads 6.0);
 //  - a page's number and address are the same for a whole wavefront and are worked out by the scalar unit (pages of 16 tokens and more);
 //  - scores are made transposed, S^T = K Q^T: the accumulator then holds, for the query of a lane's column, four tokens of each 16, which
 //    is what the second product O^T = V^T P^T wants as its right operand if its 32 tokens are taken in the order (16-token
@@ -79,7 +79,7 @@ typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
 __device__ __forceinline__ int32_t load_scalar(const int32_t *p) { return *(ScalarInts)(uintptr_t)p; }
 
 // single elements of a row, two to a register; zeros past the head
-template <typename T> __device__ __forceinline__ uint32_t load_two(const char *row, int d, int head_dim) {
+__device__ __forceinline__ uint32_t load_two(const char *row, int d, int head_dim) {
   const uint16_t *e = reinterpret_cast<const uint16_t *>(row);
   const uint32_t lo = d < head_dim ? e[d] : 0, hi = d + 1 < head_dim ? e[d + 1] : 0;
   return lo | hi << 16;
@@ -127,7 +127,7 @@ template <typename T, int kDim, int kMode, bool kLanes, bool kOnce> struct Reade
       q[s] = u32x4{};
       if constexpr (kMode == kElements) {
         if (row < rows)
-          for (int e = 0; e < 4; ++e) q[s][e] = load_two<T>(from, d + 2 * e, p.head_dim);
+          for (int e = 0; e < 4; ++e) q[s][e] = load_two(from, d + 2 * e, p.head_dim);
       } else if (row < rows && (kMode == kWhole || d < p.head_dim)) {
         q[s] = *reinterpret_cast<const u32x4 *>(from + 2 * d);
       }
@@ -188,7 +188,7 @@ template <typename T, int kDim, int kMode, bool kLanes, bool kOnce> struct Reade
       for (int s = 0; s < kSteps; ++s) {
         const int d = 32 * s + 8 * grp;
         if constexpr (kMode == kElements) {
-          for (int e = 0; e < 4; ++e) k[h][s][e] = load_two<T>(row - 16 * grp, d + 2 * e, p.head_dim);
+          for (int e = 0; e < 4; ++e) k[h][s][e] = load_two(row - 16 * grp, d + 2 * e, p.head_dim);
         } else if constexpr (kMode == kPieces) {
           k[h][s] = u32x4{};
           if (d < p.head_dim) k[h][s] = load16(row + k_lane + 64 * s);
@@ -205,7 +205,7 @@ template <typename T, int kDim, int kMode, bool kLanes, bool kOnce> struct Reade
       for (int i = 0; i < 4; ++i) {
         const char *row = kLanes ? p.v + at.v[h] + i * p.token_bytes : p.v + at.v[h] + v_lane[i];
         if constexpr (kMode == kElements) {
-          for (int e = 0; e < kOwn / 2; ++e) v[4 * h + i][e] = load_two<T>(row - 2 * kOwn * col, kOwn * col + 2 * e, p.head_dim);
+          for (int e = 0; e < kOwn / 2; ++e) v[4 * h + i][e] = load_two(row - 2 * kOwn * col, kOwn * col + 2 * e, p.head_dim);
         } else {
           if constexpr (kLanes) row += (int)value_piece - 2 * kOwn * col;
           if constexpr (kOwn == 4) {
@@ -725,7 +725,12 @@ AttendLaunch attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool 
     return (int32_t)c;
   };
   // Prompts with many rows: a CU holds one workgroup, which takes 12 us and 30 ns a token of 128 rows (half of that for every half of the rows), and a part costs a row 0.26 ns
-  // in writing and merging.  us at 16 / 32 / 64 parts, 488 rows over 32749 tokens 84 / 52 / 61 (the sum says 77 / 51 / 71).
+  // in writing and merging.  us at 1 / 2 / 4 / 8 / 16 / 32 / 64 parts a prompt, responses of one token, and in brackets what the sum of these costs takes:
+  //   1 prompt x 2 KV heads, 488 rows of 32749 tokens  1109 / 564 / 294 / 155 / 87 / 58 / 66 (56)     1 x 8, 64 rows of 8192  147 / 81 / 47 / 30 / 22.0 / 23.1 / 31 (22.8)
+  //   8 x 8, 128 rows of 2048  91 / 59 / 45 / 55 / 79 (44)                                            2 x 32, 20 rows of 4096  56 / 41 / 39 / 45 / 57 / 73 (39)
+  //   16 x 2, 96 rows of 1024  42 / 31 / 27.3 / 28.3 (28.0)                                           32 x 8, 512 rows of 512  206 / 251 / 352 (206)
+  //   1 x 12, 40 rows of 32768, heads of 64  340 / 180 / 99 / 58 / 38 / 42 / 43 (34)                  1 x 8, 40 rows of 20000, heads of 72  265 / 141 / 79 / 46 / 30 / 27 / 32 (26)
+  // It is within 4 % of the best power of two there and on four more shapes.
   const auto chunk_of_prompts = [&](int64_t len, int64_t others, int row_waves) {
     int64_t best = 0;
     double least = 0;
@@ -756,7 +761,12 @@ AttendLaunch attend_shape(const hf_kv_cache &cache, const hf_attention &a, bool 
   s.suffix_wgs = (uint64_t)a.n_seqs * s.suffix_parts * s.suffix_blocks * cache.n_kv_heads;
   // where more workgroups than the chip holds at a time have lengths of their own (above: 94 us, 107 in the order of the sequences; 165 against 164 where all are alike)
   s.ordered = a.n_seqs <= kThreads && s.suffix_wgs > kResident && s.max_suffix > 4 * kTile * 4;
+  // A wavefront to a short response.  us, four wavefronts / one, lengths from 1 to the bound: heads of 64 and 32 up to 128 tokens 40 / 38 (6144 workgroups) and 28 / 24 (4096), up to
+  // 256 53 / 59 and 32.6 / 33.5; heads of 128 up to 32 tokens 20.9 / 18.8 (1536), up to 128 26.8 / 28.1 (1024) and 48.4 / 49.4 (4096), up to 256 33 / 37 and 66 / 75; fewer workgroups than
+  // the chip holds, up to 128 tokens, 22 / 27 (768) and, up to 64, 11.5 / 18 (128).  At heads of 128 the limit could be half of this.
   s.brief = s.suffix_wgs > kResident && s.max_suffix <= 4 * kTile;
+  // Responses behind the prompts in one grid, in workgroups as large as the prompts'.  us, a grid each / one, by the workgroups of responses: 64 22.6 / 18.0, 488 62.4 / 61.6, 576 37 / 30,
+  // 960 18.1 / 17.6; 1024 of up to 512 tokens 36 / 29, 49 / 49 and 52 / 50, of up to 2048 65 / 70, 101 / 116 and 131 / 155; 1280 57 / 53, 1920 22.6 / 23.5.  Up to 256 it was never slower.
   s.together = s.row_waves && !s.brief && s.suffix_wgs <= 256;
   if (!s.direct) s.workspace = ((size_t)a.n_seqs * a.n_q_heads * (s.prefix_parts + s.suffix_parts)) * (cache.head_dim + 2) * sizeof(float);
   // (the workspace stays as it is asked for by the parts, so that it follows from those alone)

@@ -5,13 +5,14 @@
 //
 // The forward pass reads every logit once and writes a few numbers a row; the gradient reads and writes each once.  HBM is
 // the bound of the gradient (6.2 TB/s at 4096 x 32000 bf16, read and written) and of 32-bit logits (5.6 TB/s at 2048 x 128256).  At 2 bytes an element the forward pass has
-// room for eleven vector operations on each and needs nine and a half (a base-2 exponential counts as four): 4.8 TB/s at 4096 x 32000, where vector instructions issue 70 % of
+// room for eleven vector operations on each and needs nine and a half (a base-2 exponential counts as four): 4.8 TB/s at 4096 x 32000, where vector instructions issue 71 % of
 // the time.  A workgroup takes a row; every lane keeps its own running maximum, sum and weighted sum over its vectors and
 // they are merged once at the end.
 //
 // The likeliest tokens come out of the same pass: besides its maximum a lane remembers in which of its vectors it first met it.
 // The top_n-th largest of 64 groups' maxima bounds the top_n-th largest element from below, so only lanes whose own maximum reaches that
-// bound can hold an answer; they, about top_n of them, read their vectors again (from L2) and hand over what reaches the bound.  Keys are value and
+// bound can hold an answer; they, about top_n of them, read their vectors again (from L2, of long rows from beyond it: 1226 MB are
+// fetched for the 1051 of 2048 x 128256 f32 with twenty tokens) and hand over what reaches the bound.  Keys are value and
 // position together, so they are all different and ties fall to the lower id by themselves.
 #include <hip/hip_runtime.h>
 
