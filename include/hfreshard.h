@@ -622,6 +622,137 @@ typedef struct {
 } hf_logprobs_grad;
 HF_API int hf_token_logprobs_back(const hf_logits *in, const hf_logprobs_grad *grad, void *hip_stream);
 
+/* ---- around the steps of a rollout -----------------------------------------------------
+ * What stands beside the operators above, with their conventions: logits on their way to a choice of token, the pages of
+ * a cache whose sequences end, go on and branch, and the update towards a teacher. */
+
+/* hf_adjust_logits: penalties for repeated tokens, biases, and tokens that a grammar rules out, in one pass over the logits and one launch.
+ *   seen (anywhere in the row's tokens):  x <- x > 0 ? x / repetition : x * repetition
+ *   n times in the row's answer, n > 0:   x <- x - frequency * n - presence
+ *   with a bias:                          x <- x + bias        (of several for one token the last one holds)
+ *   bit not set:                          x <- -inf            (whatever it was, NaN included)
+ * A row's tokens are tokens[r, 0 .. lens[r]-1], the first prompt_lens[r] of them its prompt and the others its answer; lengths are cut to 0 .. width.
+ * Tokens and biases of ids outside 0 .. vocab-1 do not count.  Bit j % 32 of word j / 32 of a row of `allowed` is token j's; a row of logits whose
+ * allowed_rows is outside 0 .. n_allowed-1 has none ruled out, one for which no bit is set is -inf throughout.  Computed in 32 bits, rounded once; logits that
+ * nothing applies to keep their bits. */
+typedef struct {
+  const void *logits;         /* [rows, vocab] of dtype */
+  void *out;                  /* the same shape and type; may be the logits, with the same stride: then only what changes is written */
+  const void *tokens;         /* [rows, width] of int32 or int64; may be null */
+  const int32_t *lens;        /* [rows]; null exactly if tokens is */
+  const int32_t *prompt_lens; /* [rows]; null: no prompts */
+  const float *repetition, *frequency, *presence; /* [rows]; null: 1, 0 and 0 */
+  const int32_t *bias_ids;    /* [rows, n_bias], contiguous; null if n_bias is 0 */
+  const float *bias;          /* [rows, n_bias], contiguous */
+  const uint32_t *allowed;    /* [n_allowed, (vocab + 31) / 32]; may be null */
+  const int32_t *allowed_rows; /* [rows]; null: row r has row r of allowed */
+  int64_t rows, row_stride, out_stride, tokens_stride, allowed_stride;
+  int32_t dtype;              /* HF_BF16, HF_F16 or HF_F32 */
+  int32_t vocab;              /* 1 .. 2^30 */
+  int32_t token_bytes;        /* 4 or 8 */
+  int32_t width, n_bias, n_allowed;
+} hf_adjustment;
+HF_API int hf_adjust_logits(const hf_adjustment *args, void *hip_stream);
+
+#define HF_MAX_DISTILL 256
+#define HF_DISTILL_REST 0x1u /* all tokens that are not named count together, as one more */
+/* hf_top_distill: how far rows of logits are from a teacher that is known by the log probabilities of some tokens (what hf_token_logprobs gives as
+ * top_ids and top_logprobs, say).  p = softmax of y = x * inv_temperature; q_j = exp(logprobs[r, j]) and p_j belong to token ids[r, j].  With
+ * HF_DISTILL_REST the other tokens are one more: p_rest is their sum, q_rest = max(0, 1 - sum q_j), whose logarithm is taken as that of 2^-24 at least.
+ *   loss = (1 - reverse) sum q (log q - log p)  +  reverse sum p (log p - log q)
+ * A place of the list whose id is outside 0 .. vocab-1 or whose log probability is -inf names no token, and where an id comes twice its first place counts.  A row without any named
+ * token is not read and has loss 0.  No rest is counted where no other token has p > 0 (all are named, or ruled out with -inf).  A named
+ * token with x = -inf and q > 0 makes the loss inf if reverse < 1.  A row with NaN or +inf among its logits, or NaN among its log probabilities, has NaN results.
+ * For hf_top_distill_back: norm holds the largest logit m of the tokens that are not named and log sum exp((x - m) * inv_temperature) over them, and
+ * slopes the derivative of loss by the logit of every named token and, last, what exp((x_i - m) * inv_temperature - norm[1]) is multiplied by for every other.  One launch. */
+typedef struct {
+  const int32_t *ids;    /* [rows, n], contiguous */
+  const float *logprobs; /* [rows, n], contiguous */
+  float *loss;           /* [rows]; may be null */
+  float *norm;           /* [rows, 2], contiguous; null exactly if slopes is */
+  float *slopes;         /* [rows, n + 1], contiguous; may be null */
+  int32_t n;             /* 1 .. HF_MAX_DISTILL */
+  float reverse;         /* 0 .. 1 */
+  uint32_t flags;
+  int32_t _pad;
+} hf_distillation;
+HF_API int hf_top_distill(const hf_logits *in, const hf_distillation *args, void *hip_stream); /* in->targets is null */
+
+/* hf_top_distill_back: the gradient of sum_r grad_loss[r] * loss[r] with respect to the logits, from what hf_top_distill gave for the same logits, lists,
+ * temperature and flags.  Rows without named tokens are set to 0, unread.  Other tokens with p = 0 have gradient 0.  dlogits has the logits' type and may be the
+ * logits themselves, with the same stride.  One launch. */
+typedef struct {
+  const int32_t *ids;
+  const float *norm, *slopes;
+  const float *grad_loss; /* [rows] */
+  void *dlogits;          /* [rows, vocab] */
+  int64_t dlogits_stride;
+  int32_t n, _pad;
+} hf_distillation_grad;
+HF_API int hf_top_distill_back(const hf_logits *in, const hf_distillation_grad *grad, void *hip_stream);
+
+/* The pages of a model's caches, one per layer, all alike but for k and v and apart from one another.  Whose a page is is kept in tables of page numbers (those of
+ * hf_attend: [rows, width], lengths [rows]) and in refs [n_pages], how many rows of tables name it; a page with 0 is free.  Several rows may
+ * share pages that are full, one that is not belongs to one row.  The calls below read tables, lengths and reference counts on the device and write new ones, and move
+ * whatever has to move in all caches, without a trip to the host.  Of a row's table the entries of its length count, cut to 0 .. width * page_tokens tokens; entries outside
+ * 0 .. n_pages-1 name no page and come out as -1, and so do those behind.  Free pages are taken in rising order, so that results depend on the arguments alone.
+ * refs_out may be refs; other outputs lie apart from inputs.  The workspace is 16-byte aligned, its contents do not matter and are not kept. */
+#define HF_MAX_CACHES 128
+typedef struct {
+  const hf_kv_cache *caches; /* HOST memory: [n_caches] */
+  int32_t n_caches;          /* 1 .. HF_MAX_CACHES */
+  int32_t _pad;
+} hf_page_pool;
+
+/* hf_fork_pages: row r of the result goes on where row parents[r] of the tables stands; outside 0 .. rows-1 it is empty (length 0).  Old rows that nobody continues give their pages
+ * back.  Full pages are shared.  A last page that is not full goes to the first row that continues it; each further one gets a free page (those given back by this very call among them),
+ * into which the tokens are copied.  A row for which no page is left comes out empty, and the pages that it would have shared are not counted for it. */
+typedef struct {
+  const int32_t *tables, *lens; /* [rows, width], [rows] */
+  const int32_t *parents;       /* [rows_out] */
+  const int32_t *refs;          /* [n_pages] */
+  int32_t *tables_out, *lens_out; /* [rows_out, width], [rows_out] */
+  int32_t *refs_out;
+  void *workspace;
+  size_t workspace_bytes;
+  int32_t rows, rows_out, width, _pad;
+} hf_page_fork;
+HF_API size_t hf_fork_pages_workspace_bytes(const hf_page_pool *pool, const hf_page_fork *args); /* (size_t)-1: see hf_last_error */
+HF_API int hf_fork_pages(const hf_page_pool *pool, const hf_page_fork *args, void *hip_stream);
+
+/* hf_grow_pages: room for counts[r] more tokens (cut to 0 .. most) in every row.  slots[r, i] is the place of the i-th of them, as hf_append_kv takes it; -1 behind the last and in pages that the
+ * table does not name.  Rows take their pages in order.  A row that would not fit into the table's width, or that wants more pages than are left, stays as it is, with
+ * slots of -1; behind a row that wanted more pages than were left only rows that need none grow.  tables_out may be tables and lens_out lens. */
+typedef struct {
+  const int32_t *tables, *lens;
+  const int32_t *counts; /* [rows] */
+  const int32_t *refs;
+  int32_t *tables_out, *lens_out;
+  int64_t *slots;        /* [rows, most], contiguous */
+  int32_t *refs_out;
+  void *workspace;
+  size_t workspace_bytes;
+  int32_t rows, width, most, _pad;
+} hf_page_grow;
+HF_API size_t hf_grow_pages_workspace_bytes(const hf_page_pool *pool, const hf_page_grow *args);
+HF_API int hf_grow_pages(const hf_page_pool *pool, const hf_page_grow *args, void *hip_stream);
+
+#define HF_MAX_TABLES 4
+/* hf_compact_pages: with n pages in use (refs not 0), those from number n on move to the free ones below n, the i-th of the first to the i-th of the second, so that all that is used lies in the first n
+ * pages.  places[p] is where page p is now, -1 if it was free; the entries of up to HF_MAX_TABLES arrays of page numbers are replaced by their places (entries outside 0 .. n_pages-1 stay as they are). */
+typedef struct {
+  const int32_t *refs;
+  int32_t *refs_out, *places; /* [n_pages] */
+  int32_t *live;              /* [1]: n */
+  const int32_t *entries[HF_MAX_TABLES]; /* [n_entries]; */
+  int32_t *entries_out[HF_MAX_TABLES];   /* may be the same */
+  int64_t n_entries[HF_MAX_TABLES];      /* 0: none, the pointers may be null */
+  void *workspace;
+  size_t workspace_bytes;
+} hf_page_compact;
+HF_API size_t hf_compact_pages_workspace_bytes(const hf_page_pool *pool, const hf_page_compact *args);
+HF_API int hf_compact_pages(const hf_page_pool *pool, const hf_page_compact *args, void *hip_stream);
+
 HF_API const char *hf_last_error(void);
 HF_API const char *hf_version(void);
 

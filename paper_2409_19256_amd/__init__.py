@@ -2,7 +2,7 @@
 
 `binding` mirrors the C ABI one to one; `Plan` is a thin convenience wrapper that only
 marshals arguments into those calls; `rollout` does the same for the operators that the
-actor runs between two transitions (paged cache, attention, log probabilities).  All load libhfreshard.so on first use and raise
+actor runs between two transitions (paged cache and its pages, attention, log probabilities, adjusted logits, distillation).  All load libhfreshard.so on first use and raise
 if it has not been built (`python -m paper_2409_19256_amd.build`); there is no fallback.
 """
 import importlib

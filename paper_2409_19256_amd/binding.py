@@ -47,6 +47,7 @@ HF_VARIANT_PERSISTENT, HF_VARIANT_ONE_WG_PER_TILE, HF_VARIANT_LDS_STAGED, HF_VAR
 HF_BF16, HF_F16, HF_F32 = 0, 1, 2
 HF_ROT_INTERLEAVED = 0x1
 HF_MAX_TOP = 64
+HF_MAX_DISTILL, HF_DISTILL_REST, HF_MAX_CACHES, HF_MAX_TABLES = 256, 0x1, 128, 4
 
 TENSOR_NAMES = {
     HF_T_EMBED: "embed", HF_T_LN1: "ln1", HF_T_QKV: "qkv", HF_T_O: "o", HF_T_LN2: "ln2", HF_T_GATE_UP: "gate_up",
@@ -124,6 +125,43 @@ class hf_logprobs_grad(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("norm", "entropy", "grad_logprob", "grad_entropy", "dlogits")] + [("dlogits_stride", C.c_int64)]
 
 
+class hf_adjustment(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("logits", "out", "tokens", "lens", "prompt_lens", "repetition", "frequency", "presence", "bias_ids", "bias",
+                                           "allowed", "allowed_rows")] +
+                [(n, C.c_int64) for n in ("rows", "row_stride", "out_stride", "tokens_stride", "allowed_stride")] +
+                [(n, C.c_int32) for n in ("dtype", "vocab", "token_bytes", "width", "n_bias", "n_allowed")])
+
+
+class hf_distillation(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("ids", "logprobs", "loss", "norm", "slopes")] +
+                [("n", C.c_int32), ("reverse", C.c_float), ("flags", C.c_uint32), ("_pad", C.c_int32)])
+
+
+class hf_distillation_grad(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("ids", "norm", "slopes", "grad_loss", "dlogits")] +
+                [("dlogits_stride", C.c_int64), ("n", C.c_int32), ("_pad", C.c_int32)])
+
+
+class hf_page_pool(C.Structure):
+    _fields_ = [("caches", C.POINTER(hf_kv_cache)), ("n_caches", C.c_int32), ("_pad", C.c_int32)]
+
+
+class hf_page_fork(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("tables", "lens", "parents", "refs", "tables_out", "lens_out", "refs_out", "workspace")] +
+                [("workspace_bytes", C.c_size_t)] + [(n, C.c_int32) for n in ("rows", "rows_out", "width", "_pad")])
+
+
+class hf_page_grow(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("tables", "lens", "counts", "refs", "tables_out", "lens_out", "slots", "refs_out", "workspace")] +
+                [("workspace_bytes", C.c_size_t)] + [(n, C.c_int32) for n in ("rows", "width", "most", "_pad")])
+
+
+class hf_page_compact(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("refs", "refs_out", "places", "live")] +
+                [("entries", C.c_void_p * HF_MAX_TABLES), ("entries_out", C.c_void_p * HF_MAX_TABLES), ("n_entries", C.c_int64 * HF_MAX_TABLES),
+                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)])
+
+
 hf_plan_p = C.c_void_p
 _P = hf_plan_p
 
@@ -174,6 +212,15 @@ SIGNATURES = {
     "hf_attend": (C.c_int, [C.POINTER(hf_kv_cache), C.POINTER(hf_attention), C.c_void_p]),
     "hf_token_logprobs": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_logprobs), C.c_void_p]),
     "hf_token_logprobs_back": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_logprobs_grad), C.c_void_p]),
+    "hf_adjust_logits": (C.c_int, [C.POINTER(hf_adjustment), C.c_void_p]),
+    "hf_top_distill": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_distillation), C.c_void_p]),
+    "hf_top_distill_back": (C.c_int, [C.POINTER(hf_logits), C.POINTER(hf_distillation_grad), C.c_void_p]),
+    "hf_fork_pages_workspace_bytes": (C.c_size_t, [C.POINTER(hf_page_pool), C.POINTER(hf_page_fork)]),
+    "hf_fork_pages": (C.c_int, [C.POINTER(hf_page_pool), C.POINTER(hf_page_fork), C.c_void_p]),
+    "hf_grow_pages_workspace_bytes": (C.c_size_t, [C.POINTER(hf_page_pool), C.POINTER(hf_page_grow)]),
+    "hf_grow_pages": (C.c_int, [C.POINTER(hf_page_pool), C.POINTER(hf_page_grow), C.c_void_p]),
+    "hf_compact_pages_workspace_bytes": (C.c_size_t, [C.POINTER(hf_page_pool), C.POINTER(hf_page_compact)]),
+    "hf_compact_pages": (C.c_int, [C.POINTER(hf_page_pool), C.POINTER(hf_page_compact), C.c_void_p]),
     "hf_last_error": (C.c_char_p, []),
     "hf_version": (C.c_char_p, []),
 }

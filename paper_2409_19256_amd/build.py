@@ -13,7 +13,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhfreshard.so")
 BENCH_EXE = os.path.join(PKG, "hfbench")
 TORCH_MODULE = os.path.join(PKG, "_rollout.so")
-SOURCES = ["planner.cpp", "reshard_kernels.hip", "abi.hip", "append_kernels.hip", "attend_kernels.hip", "logprob_kernels.hip", "rollout_abi.hip"]
+SOURCES = ["planner.cpp", "reshard_kernels.hip", "abi.hip", "append_kernels.hip", "attend_kernels.hip", "logprob_kernels.hip", "rollout_abi.hip",
+           "adjust_kernels.hip", "distill_kernels.hip", "page_kernels.hip", "steps_abi.hip"]
 
 
 def hipcc() -> str:
@@ -24,7 +25,7 @@ def hipcc() -> str:
 
 
 def build_library(verbose: bool = True) -> str:
-    """Compile every source for gfx950 and link the shared library; returns its path.  rollout.py's native module is built beside it where it can be."""
+    """Compile every source for gfx950 and link the shared library; returns its path.  rollout.py's native modules are built beside it where they can be."""
     cmd = [hipcc(), "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared", "-fvisibility=hidden", "-Wl,-soname,libhfreshard.so",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            # kernel arguments arrive in registers: a workgroup here lives for two or three round trips to
@@ -46,34 +47,42 @@ def build_library(verbose: bool = True) -> str:
     subprocess.run(cmd, check=True, cwd=ROOT)
     os.replace(BENCH_EXE + ".tmp", BENCH_EXE)
     try:
-        build_torch_module(verbose)
+        build_torch_modules(verbose)
     except (OSError, subprocess.CalledProcessError) as e:
         # no headers of Python's, no host compiler that torch's headers pass: the library does not need them.  An older module would not fit it.
-        if os.path.exists(TORCH_MODULE):
-            os.remove(TORCH_MODULE)
-        print(f"_rollout was not built, so that paper_2409_19256_amd.rollout cannot be imported: {e}", file=sys.stderr, flush=True)
+        for module in torch_modules().values():
+            if os.path.exists(module):
+                os.remove(module)
+        print(f"_rollout and _steps were not built, so that paper_2409_19256_amd.rollout cannot be imported: {e}", file=sys.stderr, flush=True)
     return LIB
 
 
-def build_torch_module(verbose: bool = True) -> None:
+def torch_modules() -> dict:
+    """Source and module of each of rollout.py's native parts; they lie side by side."""
+    return {"rollout_torch.cpp": TORCH_MODULE, "steps_torch.cpp": os.path.join(os.path.dirname(TORCH_MODULE), "_steps.so")}
+
+
+def build_torch_modules(verbose: bool = True) -> None:
     """rollout.py's native part: host code over torch's headers, linked against the library.  Without torch there is nothing to build it for."""
     try:
         import torch
         from torch.utils.cpp_extension import include_paths, library_paths
     except ImportError:
         return
-    cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", os.path.join(ROOT, "include")]
+    head = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", "-I", os.path.join(ROOT, "include")]
     for path in include_paths() + [sysconfig.get_paths()["include"]]:
-        cmd += ["-isystem", path]
-    cmd += [os.path.join(CSRC, "rollout_torch.cpp"), "-o", TORCH_MODULE + ".tmp", "-L", PKG, "-lhfreshard", "-Wl,-rpath,$ORIGIN"]
+        head += ["-isystem", path]
+    tail = ["-L", PKG, "-lhfreshard", "-Wl,-rpath,$ORIGIN"]
     for path in library_paths():
-        cmd += ["-L", path]
-    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True, cwd=ROOT)
-    os.replace(TORCH_MODULE + ".tmp", TORCH_MODULE)
+        tail += ["-L", path]
+    tail += ["-ltorch_python", "-ltorch_cpu", "-lc10"]
+    for source, module in torch_modules().items():
+        cmd = head + [os.path.join(CSRC, source), "-o", module + ".tmp"] + tail
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True, cwd=ROOT)
+        os.replace(module + ".tmp", module)
 
 
 if __name__ == "__main__":

@@ -1,0 +1,376 @@
+// Distillation from a teacher's top tokens: the divergence of rows of logits from it, and the gradient.
+//
+// Named tokens j with teacher's q_j and student's p_j = softmax(x / T)_j, and the rest as one more (or left out):
+//   ahead = sum q (ln q - ln p),  back = sum p (ln p - ln q),  loss = (1 - w) ahead + w back
+//   T dloss/dx_j = (1 - w) (p_j Q - q_j) + w p_j (ln p_j - ln q_j + 1 - back - P)      Q = sum q, P = sum p over what is counted
+//   and of a token i that is not named the same with its rest's numbers, times its share of it:
+//   T dloss/dx_i = e^(x_i / T) / sum of the others' e^(x / T) * ((1 - w) (p_rest Q - q_rest) + w p_rest (ln p_rest - ln q_rest + 1 - back - P))
+//
+// The forward pass reads every logit once and sums the exponentials of those that are not named: what is left of 1 beside a few likely tokens would be lost in a
+// difference of two sums.  Which are named stands in a bitmap in shared memory, a byte to a vector of 8.  The named tokens are a few numbers a row, taken in 64 bits
+// (a difference of logarithms near 1, one minus a sum of probabilities).  The gradient reads and writes every logit once; its named elements come out of a list.
+#include <hip/hip_runtime.h>
+
+#include "lanes.hpp"
+#include "logit_rows.hpp"
+#include "step_kernels.hpp"
+
+namespace hf {
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
+// tokens that the bitmap spans at a time: every row that has so few lanes, or as many as 16 KiB hold
+constexpr int window_of(int threads) { return threads == 64 ? 1 << 13 : threads == 256 ? 1 << 15 : 1 << 17; }
+
+struct Logits {
+  const void *data;
+  int64_t row_stride;
+  int32_t vocab;
+  float inv_temperature;
+};
+
+// Largest element m, and the sum over the elements of 2^d with d = (x - r) c - k, c = log2(e) / temperature.  r and k follow the first elements and then only
+// what is past them by kSlack of base 2; below kWhole r is 0 and k a whole number, so that d is one operation and sums move to another k exactly.
+struct Stats {
+  float m, r, k, s;
+};
+constexpr float kSlack = 8, kWhole = 1 << 24;
+__device__ __forceinline__ void rebase(Stats &st, float x0, float c) {
+  const bool whole = fabsf(x0 * c) < kWhole;
+  const float k = whole ? rintf(x0 * c) : 0.f, r = whole || x0 == -INFINITY ? 0.f : x0;
+  const float d = st.s == 0 ? 0.f : fmaf(st.r - r, c, st.k - k); // (nothing to move before the first element)
+  st.s *= __builtin_amdgcn_exp2f(d);
+  st.r = r;
+  st.k = k;
+}
+__device__ __forceinline__ Stats merge_wave(Stats st, float c) {
+  st.m = over_wave<Max>(st.m);
+  rebase(st, st.m, c);
+  return {st.m, st.r, st.k, over_wave<Sum>(st.s)};
+}
+template <int kN> __device__ __forceinline__ void join(Stats &st, float &limit, const float (&x)[kN], float c) {
+  float top = larger(x[0], x[1]);
+#pragma unroll
+  for (int i = 2; i < kN; i += 2) top = larger(top, x[i], x[i + 1]);
+  st.m = larger(st.m, top);
+  if (top > limit) {
+    rebase(st, top, c);
+    limit = top + kSlack / c;
+  }
+  if (st.r == 0) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) st.s += __builtin_amdgcn_exp2f(fmaf(x[i], c, -st.k)); // NaN comes through here
+  } else {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) st.s += __builtin_amdgcn_exp2f((x[i] - st.r) * c);
+  }
+}
+
+__device__ __forceinline__ double sum_wave(double x) {
+#pragma unroll
+  for (int d = kWave / 2; d; d /= 2) x += __shfl_xor(x, d);
+  return x;
+}
+// over the workgroup; `shared` holds one number a wavefront and may be used again at once
+template <int kThreads> __device__ __forceinline__ double sum_block(double x, double *shared) {
+  x = sum_wave(x);
+  if constexpr (kThreads > kWave) {
+    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = x;
+    __syncthreads();
+    x = shared[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / kWave; ++w) x += shared[w];
+    __syncthreads();
+  }
+  return x;
+}
+
+template <typename T, int kThreads> __global__ __launch_bounds__(kThreads) void top_distill(Logits in, hf_distillation a) {
+  constexpr int kWaves = kThreads / kWave, kV = kVec<T>, kBatch = 4, kWindow = window_of(kThreads);
+  constexpr int kPlaces = (HF_MAX_DISTILL + kThreads - 1) / kThreads; // of the list, to a lane
+  typedef typename Vector<T>::type V;
+  __shared__ uint32_t named[kWindow / 32];
+  __shared__ int32_t ids[HF_MAX_DISTILL];
+  __shared__ double slope_of[HF_MAX_DISTILL], shared[kWaves];
+  __shared__ Stats stats[kWaves];
+  __shared__ uint32_t any, twice;
+  const int64_t r = blockIdx.x;
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, vocab = in.vocab;
+  const T *row = static_cast<const T *>(in.data) + r * in.row_stride;
+  const float c = in.inv_temperature * kLog2e;
+
+  // the list: id (-1: names nothing), the teacher's log probability, the logit
+  int32_t given[kPlaces], id[kPlaces];
+  float lq[kPlaces], x_named[kPlaces];
+  if (t == 0) any = twice = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k) {
+    const int j = t + k * kThreads;
+    given[k] = id[k] = -1, lq[k] = 0;
+    if (j < a.n) {
+      given[k] = a.ids[r * a.n + j], lq[k] = a.logprobs[r * a.n + j];
+      if (given[k] < 0 || given[k] >= vocab) given[k] = -1;
+      else if (lq[k] != -INFINITY) id[k] = given[k];
+      ids[j] = id[k];
+      if (id[k] >= 0) any = 1;
+    }
+  }
+  __syncthreads();
+  if (!any) {
+    if (t == 0) {
+      if (a.loss) a.loss[r] = 0;
+      if (a.norm) a.norm[2 * r] = 0, a.norm[2 * r + 1] = INFINITY; // what the gradient knows such a row by
+    }
+    if (a.slopes)
+      for (int j = t; j <= a.n; j += kThreads) a.slopes[r * (a.n + 1) + j] = 0;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k) x_named[k] = given[k] >= 0 ? (float)row[given[k]] : -INFINITY;
+
+  Stats st = {-INFINITY, 0, 0, 0};
+  float limit = -INFINITY;
+  for (int window = 0; window < vocab; window += kWindow) {
+    const int size = min(kWindow, vocab - window), n_vec = size / kV;
+    for (int i = t; i < (size + 31) / 32; i += kThreads) named[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPlaces; ++k)
+      if (const int at = id[k] - window; id[k] >= 0 && at >= 0 && at < size)
+        if (atomicOr(&named[at / 32], 1u << at % 32) >> at % 32 & 1) twice = 1;
+    __syncthreads();
+    const T *from = row + window;
+    const uint8_t *bytes = reinterpret_cast<const uint8_t *>(named);
+    // kN vectors, kThreads apart from vector `at` on
+    const auto add = [&](const auto &v, int at) {
+      constexpr int kN = sizeof(v) / sizeof(v[0]);
+      float x[kN * kV];
+#pragma unroll
+      for (int k = 0; k < kN; ++k) {
+        const int i = at + k * kThreads;
+        const uint32_t bits = kV == 8 ? bytes[i] : bytes[i / 2] >> (i % 2 * 4) & 15;
+#pragma unroll
+        for (int e = 0; e < kV; ++e) x[k * kV + e] = (float)v[k][e];
+        if (bits) {
+#pragma unroll
+          for (int e = 0; e < kV; ++e) x[k * kV + e] = bits >> e & 1 ? -INFINITY : x[k * kV + e];
+        }
+      }
+      join(st, limit, x, c);
+    };
+    int i = t;
+    if (i + (kBatch - 1) * kThreads < n_vec) { // the next vectors are on their way while the present ones are added
+      V v[kBatch], next[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) v[k] = load_vec(from + (int64_t)(i + k * kThreads) * kV);
+      for (; i + (2 * kBatch - 1) * kThreads < n_vec; i += kBatch * kThreads) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) next[k] = load_vec(from + (int64_t)(i + (kBatch + k) * kThreads) * kV);
+        add(v, i);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) v[k] = next[k];
+      }
+      add(v, i);
+      i += kBatch * kThreads;
+    }
+    for (; i < n_vec; i += kThreads) {
+      const V one[1] = {load_vec(from + (int64_t)i * kV)};
+      add(one, i);
+    }
+    if (n_vec % kThreads == t && n_vec * kV < size) {
+      V last[1];
+#pragma unroll
+      for (int e = 0; e < kV; ++e) last[0][e] = n_vec * kV + e < size ? from[n_vec * kV + e] : (T)-INFINITY;
+      add(last, n_vec);
+    }
+    __syncthreads(); // the bitmap is used again, and `twice` is known
+  }
+  st = merge_wave(st, c);
+  if constexpr (kWaves > 1) {
+    if (lane == 0) stats[wave] = st;
+    __syncthreads();
+    st = merge_wave(lane < kWaves ? stats[lane] : Stats{-INFINITY, 0, 0, 0}, c);
+  }
+
+  // which place stands for a token that comes more than once: the first that names it
+  int lead[kPlaces];
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k) {
+    lead[k] = t + k * kThreads;
+    if (id[k] < 0) lead[k] = -1;
+    if (twice || (id[k] < 0 && given[k] >= 0)) { // (a place without a log probability may hold a token that another one names)
+      for (int j = a.n - 1; j >= 0; --j)
+        if (given[k] >= 0 && ids[j] == given[k]) lead[k] = j;
+    }
+  }
+  const auto leads = [&](int k) { return lead[k] == t + k * kThreads; };
+
+  // from here on of base e, in 64 bits, relative to the row's largest element
+  float top = st.m;
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k)
+    if (leads(k)) top = fmaxf(top, x_named[k]);
+  top = over_wave<Max>(top);
+  if constexpr (kWaves > 1) {
+    __syncthreads();
+    if (lane == 0) stats[wave].m = top;
+    __syncthreads();
+    top = over_wave<Max>(lane < kWaves ? stats[lane].m : -INFINITY);
+  }
+  const double inv_t = in.inv_temperature, w = a.reverse;
+  const bool others = !(st.s <= 0), rest = others && a.flags & HF_DISTILL_REST;
+  // ln of the others' sum, relative to their own largest and to the row's
+  const double log_own = others ? log((double)st.s) + ((double)st.k - ((double)st.m - st.r) * c) * kLn2 : -INFINITY;
+  const double log_others = others ? log_own + ((double)st.m - top) * inv_t : -INFINITY;
+  const auto y_of = [&](int k) { return x_named[k] == -INFINITY ? -(double)INFINITY : ((double)x_named[k] - top) * inv_t; };
+  double z = 0, q_sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k)
+    if (leads(k)) z += exp(y_of(k)), q_sum += exp((double)lq[k]);
+  z = sum_block<kThreads>(z, shared);
+  q_sum = sum_block<kThreads>(q_sum, shared);
+  const double log_z = log(z + exp(log_others));
+  const auto lp_of = [&](int k) { return x_named[k] == -INFINITY && log_z == log_z ? -(double)INFINITY : y_of(k) - log_z; };
+  const double lp_others = others ? log_others - log_z : -INFINITY, p_others = exp(lp_others);
+  const double q_rest = rest ? fmax(1 - q_sum, 0.) : 0., lq_rest = log(fmax(1 - q_sum, 0x1p-24)), p_rest = rest ? p_others : 0.;
+  double ahead = 0, back = 0, p_sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k)
+    if (leads(k)) {
+      const double lp = lp_of(k), p = exp(lp), q = exp((double)lq[k]);
+      if (q != 0) ahead += q * (lq[k] - lp);
+      if (p != 0 || lq[k] != lq[k]) back += p * (lp - lq[k]);
+      p_sum += p;
+    }
+  ahead = sum_block<kThreads>(ahead, shared);
+  back = sum_block<kThreads>(back, shared);
+  p_sum = sum_block<kThreads>(p_sum, shared) + p_rest;
+  if (rest) {
+    if (q_rest != 0) ahead += q_rest * (log(q_rest) - lp_others);
+    if (p_rest != 0) back += p_rest * (lp_others - lq_rest);
+  }
+  const double mass = q_sum + q_rest;
+  if (t == 0) {
+    // (a direction without weight has no part, inf though it may be)
+    if (a.loss) a.loss[r] = (float)((w < 1 ? (1 - w) * ahead : 0.) + (w > 0 ? w * back : 0.));
+    if (a.norm) a.norm[2 * r] = st.m, a.norm[2 * r + 1] = (float)log_own;
+  }
+  if (!a.slopes) return;
+  const auto slope = [&](double p, double q, double lp, double lq_) {
+    return inv_t * ((w < 1 ? (1 - w) * (p * mass - q) : 0.) + (w > 0 && p != 0 ? w * p * (lp - lq_ + 1 - back - p_sum) : 0.));
+  };
+  // what an unnamed token's share is multiplied by; without a rest its terms have no part
+  const double other = rest ? slope(p_others, q_rest, lp_others, lq_rest) : inv_t * p_others * ((w < 1 ? (1 - w) * mass : 0.) - (w > 0 ? w * (back + p_sum) : 0.));
+  double mine[kPlaces];
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k) {
+    mine[k] = 0;
+    const int j = t + k * kThreads;
+    if (j >= a.n || given[k] < 0) continue;
+    const double lp = lp_of(k);
+    if (leads(k)) slope_of[j] = mine[k] = slope(exp(lp), exp((double)lq[k]), lp, lq[k]);
+    else if (lead[k] < 0) mine[k] = x_named[k] == -INFINITY ? 0. : other * exp(((double)x_named[k] - st.m) * inv_t - log_own); // one of the others
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kPlaces; ++k) {
+    const int j = t + k * kThreads;
+    if (j >= a.n) continue;
+    if (given[k] >= 0 && lead[k] >= 0 && !leads(k)) mine[k] = slope_of[lead[k]];
+    a.slopes[r * (a.n + 1) + j] = (float)mine[k];
+  }
+  if (t == 0) a.slopes[r * (a.n + 1) + a.n] = (float)other;
+}
+
+constexpr int kBackThreads = 256;
+constexpr int kBackVectors = 4; // a lane's vectors
+
+// A workgroup takes one of `segments` pieces of a row.
+template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distill_back(Logits in, hf_distillation_grad g, uint32_t segments) {
+  constexpr int kV = kVec<T>, kPiece = kBackThreads * kBackVectors * kV;
+  typedef typename Vector<T>::type V;
+  __shared__ uint32_t named[kPiece / 32];
+  __shared__ T value[kPiece]; // of the named elements alone
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x / segments;
+  const int begin = blockIdx.x % segments * kPiece, size = min(kPiece, in.vocab - begin), n_vec = size / kV;
+  T *to = static_cast<T *>(g.dlogits) + r * g.dlogits_stride + begin;
+  const float m = g.norm[2 * r], log_sum = g.norm[2 * r + 1];
+  if (log_sum == INFINITY) { // no named tokens
+    for (int i = t; i < n_vec; i += kBackThreads) store_once(to + i * kV, V{});
+    if (const int i = n_vec * kV + t; t < kV && i < size) to[i] = (T)0.f;
+    return;
+  }
+  const T *row = static_cast<const T *>(in.data) + r * in.row_stride + begin;
+  V v[kBackVectors];
+#pragma unroll
+  for (int k = 0; k < kBackVectors; ++k)
+    if (t + k * kBackThreads < n_vec) v[k] = load_once(row + (t + k * kBackThreads) * kV);
+  const float scale = g.grad_loss[r], *slopes = g.slopes + r * (g.n + 1);
+  for (int i = t; i < kPiece / 32; i += kBackThreads) named[i] = 0;
+  __syncthreads();
+  for (int j = t; j < g.n; j += kBackThreads) {
+    const int64_t at = (int64_t)g.ids[r * g.n + j] - begin;
+    if (at < 0 || at >= size) continue;
+    atomicOr(&named[at / 32], 1u << at % 32);
+    value[at] = (T)(scale * slopes[j]); // where a token comes twice both places hold the same
+  }
+  __syncthreads();
+  const float factor = scale * slopes[g.n], inv_t = in.inv_temperature;
+  const float from = m == -INFINITY ? 0.f : m, less = log_sum == -INFINITY ? 0.f : log_sum; // nothing else has p > 0
+  const auto grad = [&](float x) {
+    return factor * __builtin_amdgcn_exp2f(fmaf(x - from, inv_t, -less) * kLog2e);
+  };
+  const uint8_t *bytes = reinterpret_cast<const uint8_t *>(named);
+#pragma unroll
+  for (int k = 0; k < kBackVectors; ++k) {
+    const int i = t + k * kBackThreads;
+    if (i >= n_vec) break;
+    const uint32_t bits = kV == 8 ? bytes[i] : bytes[i / 2] >> (i % 2 * 4) & 15;
+    V d;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) d[e] = (T)grad((float)v[k][e]);
+    if (bits) {
+#pragma unroll
+      for (int e = 0; e < kV; ++e)
+        if (bits >> e & 1) d[e] = value[i * kV + e];
+    }
+    store_once(to + i * kV, d);
+  }
+  if (const int i = n_vec * kV + t; t < kV && i < size) to[i] = named[i / 32] >> i % 32 & 1 ? value[i] : (T)grad((float)row[i]);
+}
+
+Logits logits_of(const hf_logits &in) { return {in.logits, in.row_stride, in.vocab, in.inv_temperature}; }
+
+template <typename T> hipError_t launch(const hf_logits &in, const hf_distillation &a, hipStream_t st) {
+  const dim3 grid((uint32_t)in.rows);
+  const int n_vec = in.vocab / kVec<T>;
+  const auto kernel = n_vec <= 512 ? top_distill<T, 64> : n_vec <= 2048 ? top_distill<T, 256> : n_vec <= 8192 ? top_distill<T, 512> : top_distill<T, 1024>;
+  return enqueue_kernel(kernel, grid, n_vec <= 512 ? 64 : n_vec <= 2048 ? 256 : n_vec <= 8192 ? 512 : 1024, st, logits_of(in), a);
+}
+
+} // namespace
+
+uint32_t distill_back_segments(const hf_logits &in) {
+  const uint32_t piece = kBackThreads * kBackVectors * (in.dtype == HF_F32 ? kVec<float> : kVec<__bf16>);
+  return (in.vocab + piece - 1) / piece;
+}
+
+int launch_top_distill(const hf_logits &in, const hf_distillation &a, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return (int)(in.dtype == HF_BF16 ? launch<__bf16>(in, a, st) : in.dtype == HF_F16 ? launch<_Float16>(in, a, st) : launch<float>(in, a, st));
+}
+
+int launch_top_distill_back(const hf_logits &in, const hf_distillation_grad &g, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const uint32_t segments = distill_back_segments(in);
+  const dim3 grid((uint32_t)(in.rows * segments));
+  const auto kernel = in.dtype == HF_BF16 ? top_distill_back<__bf16> : in.dtype == HF_F16 ? top_distill_back<_Float16> : top_distill_back<float>;
+  return (int)enqueue_kernel(kernel, grid, kBackThreads, st, logits_of(in), g, segments);
+}
+
+} // namespace hf

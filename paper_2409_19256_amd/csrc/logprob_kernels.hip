@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "lanes.hpp"
+#include "logit_rows.hpp"
 #include "rollout_kernels.hpp"
 
 namespace hf {
@@ -28,20 +29,6 @@ namespace {
 constexpr int kWave = 64;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kCandidates = 1024; // room for what reaches the bound; more go through find_by_rounds
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-template <typename T> constexpr int kVec = 16 / sizeof(T); // elements of a vector
-
-// rows begin at any element, so the address of a vector is a multiple of the element's size and no more
-template <typename T> struct Vector {
-  typedef T type __attribute__((ext_vector_type(16 / sizeof(T))));
-  typedef type any __attribute__((aligned(sizeof(T))));
-};
-template <typename T> __device__ __forceinline__ typename Vector<T>::type load_vec(const T *p) { return *reinterpret_cast<const typename Vector<T>::any *>(p); }
-// what nobody reads again soon; it leaves the caches to others
-template <typename T> __device__ __forceinline__ typename Vector<T>::type load_once(const T *p) { return __builtin_nontemporal_load(reinterpret_cast<const typename Vector<T>::any *>(p)); }
-template <typename T> __device__ __forceinline__ void store_once(T *p, typename Vector<T>::type v) { __builtin_nontemporal_store(v, reinterpret_cast<typename Vector<T>::any *>(p)); }
 
 // the order of floats as the order of unsigned numbers; -0 is 0, and every NaN comes last
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -62,18 +49,6 @@ struct Logits {
 
 __device__ __forceinline__ int64_t target_of(const Logits &in, int64_t row) {
   return in.target_bytes == 8 ? static_cast<const int64_t *>(in.targets)[row] : static_cast<const int32_t *>(in.targets)[row];
-}
-
-// The larger ones; fmaxf would first make a quiet NaN of what might be a signalling one, an operation for every element.
-__device__ __forceinline__ float larger(float a, float b) {
-  float r;
-  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
-}
-__device__ __forceinline__ float larger(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
 }
 
 // Largest element m, and sums over the elements of 2^d and of 2^d d with d = (x - r) c - k, c = log2(e) / temperature.  Up to kWhole r is 0 and k the base x0 c

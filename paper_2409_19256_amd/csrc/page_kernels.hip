@@ -1,0 +1,567 @@
+// The pages of a model's caches: sequences that are dropped, go on or branch, room for new tokens, live pages moved to the lowest places.
+//
+// First the books, then the data.  The books are reference counts and page tables: counts are changed by atomics (whole numbers, in any order the same), and what has an
+// order (the f-th free page to the f-th row that wants one) comes from sums over tiles of pages and of rows, each tile's own in one launch and everybody's in the next.  The data are copied
+// by the same launch that writes the tables; they are bound by HBM, the books by the launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "step_kernels.hpp"
+
+namespace hf {
+
+namespace {
+
+constexpr int kThreads = 256, kWave = 64, kWaves = kThreads / kWave;
+constexpr int kMostTiles = 1024; // whose sums a workgroup adds up by itself
+constexpr int kPageTile = 1024, kRowTile = 256;
+
+__host__ __device__ constexpr int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
+// items of a tile, a multiple of `least`
+int64_t tile_of(int64_t n, int64_t least) { return least * std::max<int64_t>(1, up(up(n, kMostTiles), least)); }
+
+// sums in front of every lane's x, and over the workgroup; `shared` holds one number a wavefront and may be used again at once
+__device__ __forceinline__ int64_t sum_before(int64_t x, int64_t *shared, int64_t *all) {
+  int64_t upto = x;
+  for (int d = 1; d < kWave; d *= 2) {
+    const int64_t y = __shfl_up((long long)upto, d);
+    if ((int)threadIdx.x % kWave >= d) upto += y;
+  }
+  if (threadIdx.x % kWave == kWave - 1) shared[threadIdx.x / kWave] = upto;
+  __syncthreads();
+  int64_t base = 0, total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < (int)threadIdx.x / kWave) base += shared[w];
+    total += shared[w];
+  }
+  __syncthreads();
+  *all = total;
+  return base + upto - x;
+}
+__device__ __forceinline__ int64_t sum_block(int64_t x, int64_t *shared) {
+  int64_t all;
+  sum_before(x, shared, &all);
+  return all;
+}
+__device__ __forceinline__ int64_t sum_of(const int64_t *sums, int64_t n, int64_t *shared) {
+  int64_t x = 0;
+  for (int64_t i = threadIdx.x; i < n; i += kThreads) x += sums[i];
+  return sum_block(x, shared);
+}
+
+// Tables of page numbers, and what of a row counts.
+struct Tables {
+  const int32_t *entries, *lens;
+  int32_t rows, width, shift; // page_tokens = 2^shift
+  int32_t n_pages;
+};
+__device__ __forceinline__ int64_t len_of(const Tables &t, int64_t row) { return min((int64_t)max(t.lens[row], 0), (int64_t)t.width << t.shift); }
+__device__ __forceinline__ int64_t pages_of(const Tables &t, int64_t len) { return (len + (1 << t.shift) - 1) >> t.shift; }
+__device__ __forceinline__ int32_t page_at(const Tables &t, int64_t row, int64_t i) {
+  const int32_t p = t.entries[row * t.width + i];
+  return p >= 0 && p < t.n_pages ? p : -1;
+}
+
+// ---- the data ------------------------------------------------------------------------------------------------------------
+
+// How the tokens of a page lie in a cache, in accesses: runs of `inner`, of which there are outer * middle.  One of the three grows with the number of tokens.
+struct Shape {
+  int64_t page, outer_stride, middle_stride; // in accesses
+  int32_t outer, middle, inner;
+  int32_t growing; // 0: outer, 1: middle, 2: inner
+};
+struct Buffers {
+  void *at[2 * HF_MAX_CACHES];
+  int32_t n;
+};
+
+template <int kVecBytes> struct Access;
+template <> struct Access<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Access<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Access<4> { typedef uint32_t type; };
+template <> struct Access<2> { typedef uint16_t type; };
+
+constexpr int kInFlight = 4;
+
+// Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.
+template <int kVecBytes> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, int64_t part) {
+  typedef typename Access<kVecBytes>::type V;
+  const uint32_t outer = s.growing == 0 ? tokens : s.outer, middle = s.growing == 1 ? tokens : s.middle, inner = s.growing == 2 ? s.inner * tokens : s.inner;
+  const uint64_t n = (uint64_t)outer * middle * inner;
+  V *base = static_cast<V *>(buffer);
+  uint64_t at = part * (kThreads * kInFlight) + threadIdx.x;
+  int64_t off[kInFlight];
+  V v[kInFlight];
+#pragma unroll
+  for (int k = 0; k < kInFlight; ++k, at += kThreads) {
+    if (at >= n) break;
+    const uint32_t run = (uint32_t)at / inner, x = (uint32_t)at % inner;
+    off[k] = run / middle * s.outer_stride + run % middle * s.middle_stride + x;
+    v[k] = base[src * s.page + off[k]];
+  }
+  at = part * (kThreads * kInFlight) + threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < kInFlight; ++k, at += kThreads) {
+    if (at >= n) break;
+    base[dst * s.page + off[k]] = v[k];
+  }
+}
+
+// ---- fork ----------------------------------------------------------------------------------------------------------------
+
+struct Fork {
+  Tables from;
+  const int32_t *parents, *refs;
+  int32_t *tables_out, *lens_out, *refs_out;
+  int32_t rows_out;
+  // workspace
+  int32_t *first;            // [n_pages] the first row that goes on in a page that is not full
+  int64_t *free_sums, *want_sums; // per tile of pages, of rows
+  int32_t *free_list;        // [rows_out]
+  int32_t *want;             // [rows_out] which free page a row wants; -1 none
+  int32_t *wanting;          // [rows_out] the rows that want one
+  int64_t *totals;           // free pages, wanted pages
+  int32_t page_tiles, row_tiles;
+  int64_t page_tile, row_tile;
+};
+__device__ __forceinline__ int64_t parent_of(const Fork &f, int64_t row) {
+  const int32_t p = f.parents[row];
+  return p >= 0 && p < f.from.rows ? p : -1;
+}
+// the page that a row goes on in, if it is not full: else -1
+__device__ __forceinline__ int32_t open_page(const Fork &f, int64_t parent) {
+  if (parent < 0) return -1;
+  const int64_t len = len_of(f.from, parent);
+  return len & ((1 << f.from.shift) - 1) ? page_at(f.from, parent, len >> f.from.shift) : -1;
+}
+__device__ __forceinline__ bool is_free(const Fork &f, int64_t page) { return f.refs_out[page] == 0 && f.first[page] == INT32_MAX; }
+
+__global__ __launch_bounds__(kThreads) void fork_begin(Fork f) {
+  for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < f.from.n_pages; i += (int64_t)gridDim.x * kThreads) {
+    if (f.refs_out != f.refs) f.refs_out[i] = f.refs[i];
+    f.first[i] = INT32_MAX;
+  }
+}
+// a wavefront to a row: old rows give their pages back, new ones take theirs
+__global__ __launch_bounds__(kThreads) void fork_count(Fork f) {
+  const int lane = threadIdx.x % kWave;
+  for (int64_t i = blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave; i < (int64_t)f.from.rows + f.rows_out; i += (int64_t)gridDim.x * kWaves) {
+    const bool old = i < f.from.rows;
+    const int64_t r = old ? i : i - f.from.rows, row = old ? r : parent_of(f, r);
+    if (row < 0) continue;
+    const int64_t len = len_of(f.from, row), n = old ? pages_of(f.from, len) : len >> f.from.shift;
+    for (int64_t k = lane; k < n; k += kWave)
+      if (const int32_t p = page_at(f.from, row, k); p >= 0) atomicAdd(&f.refs_out[p], old ? -1 : 1);
+    if (!old && lane == 0)
+      if (const int32_t p = open_page(f, row); p >= 0) atomicMin(&f.first[p], (int32_t)r);
+  }
+}
+__global__ __launch_bounds__(kThreads) void fork_sums(Fork f) {
+  __shared__ int64_t shared[kWaves];
+  int64_t n = 0;
+  if ((int)blockIdx.x < f.page_tiles) {
+    const int64_t begin = blockIdx.x * f.page_tile, end = min(begin + f.page_tile, (int64_t)f.from.n_pages);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) n += is_free(f, i);
+    n = sum_block(n, shared);
+    if (threadIdx.x == 0) f.free_sums[blockIdx.x] = n;
+  } else {
+    const int64_t tile = blockIdx.x - f.page_tiles, begin = tile * f.row_tile, end = min(begin + f.row_tile, (int64_t)f.rows_out);
+    for (int64_t r = begin + threadIdx.x; r < end; r += kThreads) {
+      const int32_t p = open_page(f, parent_of(f, r));
+      n += p >= 0 && f.first[p] != r;
+    }
+    n = sum_block(n, shared);
+    if (threadIdx.x == 0) f.want_sums[tile] = n;
+  }
+}
+__global__ __launch_bounds__(kThreads) void fork_lists(Fork f) {
+  __shared__ int64_t shared[kWaves];
+  int64_t all;
+  if ((int)blockIdx.x < f.page_tiles) {
+    int64_t base = sum_of(f.free_sums, blockIdx.x, shared);
+    const int64_t begin = blockIdx.x * f.page_tile, end = min(begin + f.page_tile, (int64_t)f.from.n_pages);
+    for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
+      const int64_t i = i0 + threadIdx.x;
+      const bool is = i < end && is_free(f, i);
+      const int64_t at = base + sum_before(is, shared, &all);
+      if (is && at < f.rows_out) f.free_list[at] = (int32_t)i;
+      if (i < end && f.first[i] != INT32_MAX) ++f.refs_out[i];
+      base += all;
+    }
+    if ((int)blockIdx.x == f.page_tiles - 1 && threadIdx.x == 0) f.totals[0] = base;
+  } else {
+    const int64_t tile = blockIdx.x - f.page_tiles, begin = tile * f.row_tile, end = min(begin + f.row_tile, (int64_t)f.rows_out);
+    int64_t base = sum_of(f.want_sums, tile, shared);
+    for (int64_t r0 = begin; r0 < end; r0 += kThreads) {
+      const int64_t r = r0 + threadIdx.x;
+      const int32_t p = r < end ? open_page(f, parent_of(f, r)) : -1;
+      const bool wants = p >= 0 && f.first[p] != r;
+      const int64_t at = base + sum_before(wants, shared, &all);
+      if (r < end) f.want[r] = wants ? (int32_t)at : -1;
+      if (wants) f.wanting[at] = (int32_t)r;
+      base += all;
+    }
+    if (tile == f.row_tiles - 1 && threadIdx.x == 0) f.totals[1] = base;
+  }
+}
+template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, int32_t row_wgs, int32_t parts) {
+  const int64_t free = f.totals[0];
+  if ((int)blockIdx.x < row_wgs) { // a wavefront to a row
+    const int lane = threadIdx.x % kWave;
+    for (int64_t r = blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave; r < f.rows_out; r += (int64_t)row_wgs * kWaves) {
+      const int64_t parent = parent_of(f, r), len = parent < 0 ? 0 : len_of(f.from, parent), n = pages_of(f.from, len);
+      const int32_t want = f.want[r];
+      const bool lost = want >= free;
+      const int32_t fresh = want >= 0 && !lost ? f.free_list[want] : -1;
+      for (int64_t k = lane; k < f.from.width; k += kWave) {
+        int32_t p = k < n ? page_at(f.from, parent, k) : -1;
+        if (lost) {
+          if (p >= 0 && k < n - 1) atomicAdd(&f.refs_out[p], -1);
+          p = -1;
+        } else if (fresh >= 0 && k == n - 1) {
+          p = fresh;
+          f.refs_out[p] = 1;
+        }
+        f.tables_out[r * f.from.width + k] = p;
+      }
+      if (lane == 0) f.lens_out[r] = lost ? 0 : (int32_t)len;
+    }
+    return;
+  }
+  const int64_t pairs = min(free, f.totals[1]), items = pairs * buffers.n * parts;
+  for (int64_t i = (int64_t)blockIdx.x - row_wgs; i < items; i += gridDim.x - row_wgs) {
+    const int64_t part = i % parts, b = i / parts % buffers.n, k = i / parts / buffers.n;
+    const int64_t parent = parent_of(f, f.wanting[k]);
+    copy_part<kVecBytes>(buffers.at[b], shape, open_page(f, parent), f.free_list[k], len_of(f.from, parent) & ((1 << f.from.shift) - 1), part);
+  }
+}
+
+// ---- grow ----------------------------------------------------------------------------------------------------------------
+
+struct Grow {
+  Tables from;
+  const int32_t *counts, *refs;
+  int32_t *tables_out, *lens_out, *refs_out;
+  int64_t *slots;
+  int32_t most;
+  // workspace
+  int64_t *free_sums, *want_sums, *before; // before [rows]: pages that the rows in front want
+  int32_t *free_list;
+  int64_t *totals;
+  int64_t list; // most free pages that can be wanted
+  int32_t page_tiles, row_tiles;
+  int64_t page_tile, row_tile;
+};
+struct Growth {
+  int64_t len, have, want; // tokens, pages, pages wanted in all
+  int32_t count;
+  bool fits;
+  __device__ int64_t need() const { return fits ? want - have : 0; }
+};
+__device__ __forceinline__ Growth growth_of(const Grow &g, int64_t row) {
+  Growth x;
+  x.len = len_of(g.from, row), x.have = pages_of(g.from, x.len);
+  x.count = min(max(g.counts[row], 0), g.most);
+  x.want = pages_of(g.from, x.len + x.count);
+  x.fits = x.want <= g.from.width && x.len + x.count <= INT32_MAX;
+  return x;
+}
+
+__global__ __launch_bounds__(kThreads) void grow_sums(Grow g) {
+  __shared__ int64_t shared[kWaves];
+  int64_t n = 0;
+  if ((int)blockIdx.x < g.page_tiles) {
+    const int64_t begin = blockIdx.x * g.page_tile, end = min(begin + g.page_tile, (int64_t)g.from.n_pages);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
+      const int32_t refs = g.refs[i];
+      n += refs == 0;
+      if (g.refs_out != g.refs) g.refs_out[i] = refs;
+    }
+    n = sum_block(n, shared);
+    if (threadIdx.x == 0) g.free_sums[blockIdx.x] = n;
+  } else {
+    const int64_t tile = blockIdx.x - g.page_tiles, begin = tile * g.row_tile, end = min(begin + g.row_tile, (int64_t)g.from.rows);
+    for (int64_t r = begin + threadIdx.x; r < end; r += kThreads) n += growth_of(g, r).need();
+    n = sum_block(n, shared);
+    if (threadIdx.x == 0) g.want_sums[tile] = n;
+  }
+}
+__global__ __launch_bounds__(kThreads) void grow_lists(Grow g) {
+  __shared__ int64_t shared[kWaves];
+  int64_t all;
+  if ((int)blockIdx.x < g.page_tiles) {
+    int64_t base = sum_of(g.free_sums, blockIdx.x, shared);
+    const int64_t begin = blockIdx.x * g.page_tile, end = min(begin + g.page_tile, (int64_t)g.from.n_pages);
+    for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
+      const int64_t i = i0 + threadIdx.x;
+      const bool is = i < end && g.refs_out[i] == 0;
+      const int64_t at = base + sum_before(is, shared, &all);
+      if (is && at < g.list) g.free_list[at] = (int32_t)i;
+      base += all;
+    }
+    if ((int)blockIdx.x == g.page_tiles - 1 && threadIdx.x == 0) g.totals[0] = base;
+  } else {
+    const int64_t tile = blockIdx.x - g.page_tiles, begin = tile * g.row_tile, end = min(begin + g.row_tile, (int64_t)g.from.rows);
+    int64_t base = sum_of(g.want_sums, tile, shared);
+    for (int64_t r0 = begin; r0 < end; r0 += kThreads) {
+      const int64_t r = r0 + threadIdx.x;
+      const int64_t at = base + sum_before(r < end ? growth_of(g, r).need() : 0, shared, &all);
+      if (r < end) g.before[r] = at;
+      base += all;
+    }
+  }
+}
+// a wavefront to a row
+__global__ __launch_bounds__(kThreads) void grow_apply(Grow g) {
+  const int lane = threadIdx.x % kWave, page_tokens = 1 << g.from.shift;
+  const int64_t free = g.totals[0];
+  for (int64_t r = blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave; r < g.from.rows; r += (int64_t)gridDim.x * kWaves) {
+    const Growth x = growth_of(g, r);
+    const int64_t before = g.before[r];
+    const bool ok = x.fits && (x.need() == 0 || before + x.need() <= free);
+    const int32_t open = x.len % page_tokens ? page_at(g.from, r, x.have - 1) : -1; // the page that the first new tokens go to
+    for (int64_t k = lane; k < g.from.width; k += kWave) {
+      int32_t p = k < x.have ? page_at(g.from, r, k) : -1;
+      if (ok && k >= x.have && k < x.want) {
+        p = g.free_list[before + k - x.have];
+        g.refs_out[p] = 1;
+      }
+      g.tables_out[r * g.from.width + k] = p;
+    }
+    for (int64_t i = lane; i < g.most; i += kWave) {
+      const int64_t at = x.len + i, k = at >> g.from.shift;
+      int64_t slot = -1;
+      if (ok && i < x.count) {
+        const int64_t p = k < x.have ? open : g.free_list[before + k - x.have];
+        if (p >= 0) slot = (p << g.from.shift) + (at & (page_tokens - 1));
+      }
+      g.slots[r * g.most + i] = slot;
+    }
+    if (lane == 0) g.lens_out[r] = (int32_t)(ok ? x.len + x.count : x.len);
+  }
+}
+
+// ---- compact -------------------------------------------------------------------------------------------------------------
+
+struct Compact {
+  const int32_t *refs;
+  int32_t *refs_out, *places, *live;
+  const int32_t *entries[HF_MAX_TABLES];
+  int32_t *entries_out[HF_MAX_TABLES];
+  int64_t n_entries[HF_MAX_TABLES];
+  // workspace
+  int64_t *live_sums;
+  int32_t *from, *to; // [n_pages / 2]
+  int64_t *totals;    // pairs
+  int32_t n_pages, page_tiles;
+  int64_t page_tile;
+};
+
+__global__ __launch_bounds__(kThreads) void compact_sums(Compact c) {
+  __shared__ int64_t shared[kWaves];
+  const int64_t begin = blockIdx.x * c.page_tile, end = min(begin + c.page_tile, (int64_t)c.n_pages);
+  int64_t n = 0;
+  for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) n += c.refs[i] != 0;
+  n = sum_block(n, shared);
+  if (threadIdx.x == 0) c.live_sums[blockIdx.x] = n;
+}
+__global__ __launch_bounds__(kThreads) void compact_lists(Compact c) {
+  __shared__ int64_t shared[kWaves];
+  const int64_t live = sum_of(c.live_sums, c.page_tiles, shared);
+  // those in use below number `live`, which stay
+  const int64_t whole = live / c.page_tile;
+  int64_t stay = 0, all;
+  for (int64_t i = whole * c.page_tile + threadIdx.x; i < live; i += kThreads) stay += c.refs[i] != 0;
+  stay = sum_block(stay, shared) + sum_of(c.live_sums, whole, shared);
+  int64_t base = sum_of(c.live_sums, blockIdx.x, shared);
+  const int64_t begin = blockIdx.x * c.page_tile, end = min(begin + c.page_tile, (int64_t)c.n_pages);
+  for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
+    const int64_t i = i0 + threadIdx.x;
+    const bool is = i < end && c.refs[i] != 0;
+    const int64_t before = base + sum_before(is, shared, &all); // in use in front of page i
+    if (i < end) {
+      if (is && i >= live) c.from[before - stay] = (int32_t)i;
+      if (!is && i < live) c.to[i - before] = (int32_t)i;
+      c.places[i] = is && i < live ? (int32_t)i : -1;
+    }
+    base += all;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) c.totals[0] = live - stay, *c.live = (int32_t)live;
+}
+// the counts of pages that stay, and those that move with theirs
+__global__ __launch_bounds__(kThreads) void compact_refs(Compact c) {
+  const int64_t pairs = c.totals[0], live = *c.live;
+  for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < c.n_pages; i += (int64_t)gridDim.x * kThreads) {
+    if (c.refs_out != c.refs && (i < live) == (c.refs[i] != 0)) c.refs_out[i] = c.refs[i];
+    if (i < pairs) {
+      const int32_t from = c.from[i], to = c.to[i], refs = c.refs[from];
+      c.refs_out[to] = refs;
+      c.refs_out[from] = 0;
+      c.places[from] = to;
+    }
+  }
+}
+template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, int32_t entry_wgs, int32_t parts) {
+  if ((int)blockIdx.x < entry_wgs) {
+    for (int k = 0; k < HF_MAX_TABLES; ++k)
+      for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < c.n_entries[k]; i += (int64_t)entry_wgs * kThreads) {
+        const int32_t p = c.entries[k][i];
+        c.entries_out[k][i] = p >= 0 && p < c.n_pages ? c.places[p] : p;
+      }
+    return;
+  }
+  const int64_t items = c.totals[0] * buffers.n * parts;
+  for (int64_t i = (int64_t)blockIdx.x - entry_wgs; i < items; i += gridDim.x - entry_wgs) {
+    const int64_t part = i % parts, b = i / parts % buffers.n, k = i / parts / buffers.n;
+    copy_part<kVecBytes>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
+  }
+}
+
+// ---- on the host ---------------------------------------------------------------------------------------------------------
+
+int shift_of(int64_t n) { // n = 2^s
+  int s = 0;
+  while ((int64_t(1) << s) < n) ++s;
+  return s;
+}
+
+Shape shape_of(const hf_kv_cache &c, int vec) {
+  Shape s = {c.page_stride / vec, 0, 0, 1, 1, c.head_dim / vec, 1};
+  const int64_t heads = c.n_kv_heads, dim = c.head_dim;
+  if (c.token_stride == dim || c.page_tokens == 1) { // a head's tokens in one run
+    s.outer = (int32_t)heads, s.outer_stride = c.head_stride / vec, s.growing = 2;
+  } else if (c.head_stride == dim || heads == 1) { // a token's heads in one run
+    s.inner = (int32_t)(heads * dim / vec);
+    if (c.token_stride == heads * dim) s.growing = 2;
+    else s.growing = 0, s.outer_stride = c.token_stride / vec;
+  } else {
+    s.outer = (int32_t)heads, s.outer_stride = c.head_stride / vec, s.middle_stride = c.token_stride / vec, s.growing = 1;
+  }
+  return s;
+}
+Buffers buffers_of(const hf_page_pool &pool) {
+  Buffers b = {};
+  for (int i = 0; i < pool.n_caches; ++i) b.at[b.n++] = pool.caches[i].k, b.at[b.n++] = pool.caches[i].v;
+  return b;
+}
+int32_t parts_of(const hf_kv_cache &c, int vec) { return (int32_t)up((int64_t)c.n_kv_heads * c.page_tokens * c.head_dim / vec, kThreads * kInFlight); }
+constexpr int64_t kMostCopyWgs = 4096, kMostRowWgs = 2048;
+
+// arrays of a workspace, one after another, each 16-byte aligned
+struct Room {
+  char *at;
+  size_t size = 0;
+  template <typename T> T *take(int64_t n) {
+    T *p = reinterpret_cast<T *>(at + size);
+    size += up(n * sizeof(T), 16) * 16;
+    return p;
+  }
+};
+Tables tables_of(const hf_page_pool &pool, const int32_t *entries, const int32_t *lens, int32_t rows, int32_t width) {
+  const hf_kv_cache &c = pool.caches[0];
+  return {entries, lens, rows, width, shift_of(c.page_tokens), (int32_t)c.n_pages};
+}
+Fork fork_of(const hf_page_pool &pool, const hf_page_fork &a, Room &room) {
+  Fork f = {tables_of(pool, a.tables, a.lens, a.rows, a.width), a.parents, a.refs, a.tables_out, a.lens_out, a.refs_out, a.rows_out};
+  f.page_tile = tile_of(f.from.n_pages, kPageTile), f.row_tile = tile_of(a.rows_out, kRowTile);
+  f.page_tiles = (int32_t)up(f.from.n_pages, f.page_tile), f.row_tiles = (int32_t)up(a.rows_out, f.row_tile);
+  f.first = room.take<int32_t>(f.from.n_pages);
+  f.free_sums = room.take<int64_t>(f.page_tiles);
+  f.want_sums = room.take<int64_t>(f.row_tiles);
+  f.free_list = room.take<int32_t>(a.rows_out);
+  f.want = room.take<int32_t>(a.rows_out);
+  f.wanting = room.take<int32_t>(a.rows_out);
+  f.totals = room.take<int64_t>(2);
+  return f;
+}
+Grow grow_of(const hf_page_pool &pool, const hf_page_grow &a, Room &room) {
+  Grow g = {tables_of(pool, a.tables, a.lens, a.rows, a.width), a.counts, a.refs, a.tables_out, a.lens_out, a.refs_out, a.slots, a.most};
+  g.page_tile = tile_of(g.from.n_pages, kPageTile), g.row_tile = tile_of(a.rows, kRowTile);
+  g.page_tiles = (int32_t)up(g.from.n_pages, g.page_tile), g.row_tiles = (int32_t)up(a.rows, g.row_tile);
+  const int64_t each = std::min<int64_t>(a.width, up(a.most, int64_t(1) << g.from.shift)); // a row's fresh pages, at most
+  g.list = std::min<int64_t>(g.from.n_pages, a.rows * each);
+  g.free_sums = room.take<int64_t>(g.page_tiles);
+  g.want_sums = room.take<int64_t>(g.row_tiles);
+  g.before = room.take<int64_t>(a.rows);
+  g.free_list = room.take<int32_t>(g.list);
+  g.totals = room.take<int64_t>(1);
+  return g;
+}
+Compact compact_of(const hf_page_pool &pool, const hf_page_compact &a, Room &room) {
+  Compact c = {a.refs, a.refs_out, a.places, a.live};
+  for (int k = 0; k < HF_MAX_TABLES; ++k) c.entries[k] = a.entries[k], c.entries_out[k] = a.entries_out[k], c.n_entries[k] = a.n_entries[k];
+  c.n_pages = (int32_t)pool.caches[0].n_pages;
+  c.page_tile = tile_of(c.n_pages, kPageTile), c.page_tiles = (int32_t)up(c.n_pages, c.page_tile);
+  c.live_sums = room.take<int64_t>(c.page_tiles);
+  c.from = room.take<int32_t>(c.n_pages / 2);
+  c.to = room.take<int32_t>(c.n_pages / 2);
+  c.totals = room.take<int64_t>(1);
+  return c;
+}
+
+template <typename F> hipError_t by_access(int vec, const F &go) {
+  return vec == 8 ? go(std::integral_constant<int, 16>{}) : vec == 4 ? go(std::integral_constant<int, 8>{}) : vec == 2 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
+}
+
+} // namespace
+
+size_t fork_workspace(const hf_page_pool &pool, const hf_page_fork &a) {
+  Room room = {nullptr};
+  fork_of(pool, a, room);
+  return room.size;
+}
+size_t grow_workspace(const hf_page_pool &pool, const hf_page_grow &a) {
+  Room room = {nullptr};
+  grow_of(pool, a, room);
+  return room.size;
+}
+size_t compact_workspace(const hf_page_pool &pool, const hf_page_compact &a) {
+  Room room = {nullptr};
+  compact_of(pool, a, room);
+  return room.size;
+}
+
+int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Room room = {static_cast<char *>(a.workspace)};
+  const Fork f = fork_of(pool, a, room);
+  const auto wgs = [](int64_t n, int64_t each) { return dim3((uint32_t)std::max<int64_t>(1, std::min(up(n, each), kMostRowWgs))); };
+  if (const hipError_t e = enqueue_kernel(fork_begin, wgs(f.from.n_pages, kThreads), kThreads, st, f)) return e;
+  if (const hipError_t e = enqueue_kernel(fork_count, wgs((int64_t)a.rows + a.rows_out, kWaves), kThreads, st, f)) return e;
+  if (const hipError_t e = enqueue_kernel(fork_sums, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
+  if (const hipError_t e = enqueue_kernel(fork_lists, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
+  const int32_t parts = parts_of(pool.caches[0], vec), row_wgs = wgs(a.rows_out, kWaves).x;
+  const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
+  return by_access(vec, [&](auto bytes) {
+    return enqueue_kernel(fork_apply<decltype(bytes)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape_of(pool.caches[0], vec), row_wgs, parts);
+  });
+}
+
+int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Room room = {static_cast<char *>(a.workspace)};
+  const Grow g = grow_of(pool, a, room);
+  if (const hipError_t e = enqueue_kernel(grow_sums, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
+  if (const hipError_t e = enqueue_kernel(grow_lists, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
+  return enqueue_kernel(grow_apply, dim3((uint32_t)std::min(up(a.rows, kWaves), kMostRowWgs)), kThreads, st, g);
+}
+
+int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, int vec, void *stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Room room = {static_cast<char *>(a.workspace)};
+  const Compact c = compact_of(pool, a, room);
+  if (const hipError_t e = enqueue_kernel(compact_sums, dim3(c.page_tiles), kThreads, st, c)) return e;
+  if (const hipError_t e = enqueue_kernel(compact_lists, dim3(c.page_tiles), kThreads, st, c)) return e;
+  if (const hipError_t e = enqueue_kernel(compact_refs, dim3((uint32_t)std::min(up(c.n_pages, kThreads), kMostRowWgs)), kThreads, st, c)) return e;
+  int64_t most = 0;
+  for (const int64_t n : c.n_entries) most = std::max(most, n);
+  const int32_t parts = parts_of(pool.caches[0], vec), entry_wgs = (int32_t)std::min(up(most, kThreads), kMostRowWgs);
+  const int64_t copies = std::max<int64_t>(1, std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs));
+  return by_access(vec, [&](auto bytes) {
+    return enqueue_kernel(compact_apply<decltype(bytes)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape_of(pool.caches[0], vec),
+                          pool.caches[0].page_tokens, entry_wgs, parts);
+  });
+}
+
+} // namespace hf

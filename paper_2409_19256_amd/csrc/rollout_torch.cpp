@@ -1,139 +1,9 @@
 // Python module _rollout: the rollout operators' C calls with torch tensors as arguments.  It looks tensors over, makes the outputs that were not
 // given, makes their GPU the current one, and fills the argument structs; the smallest calls wait for the host, and in Python this took two to three times as long as the launch (one step
 // of the tiny decoder's attention 15.8 us a call in Python).  rollout.py documents the functions and is what callers import.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
-#include <c10/core/DeviceGuard.h>
-#include <c10/core/GradMode.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <cmath>
-
-#include "hfreshard.h"
+#include "torch_args.hpp"
 
 namespace {
-
-using at::Tensor;
-
-PyObject *g_error = nullptr; // HfError(code, name of the call)
-
-struct Wrong {
-  const char *name, *what;
-};
-
-// the tensor of an argument, null for None; throws Wrong
-const Tensor *given(PyObject *o, const char *name) {
-  if (o == Py_None) return nullptr;
-  if (!THPVariable_Check(o)) throw Wrong{name, "a tensor is wanted"};
-  return &THPVariable_Unpack(o);
-}
-const Tensor &wanted(PyObject *o, const char *name) {
-  const Tensor *t = given(o, name);
-  if (!t) throw Wrong{name, "a tensor is wanted"};
-  return *t;
-}
-
-// address of a contiguous tensor of a type and shape on the GPU `device`; null for none
-template <size_t kN> void *whole(const Tensor *t, const char *name, at::ScalarType type, const int64_t (&shape)[kN], int device) {
-  if (!t) return nullptr;
-  if (!t->is_cuda() || t->get_device() != device) throw Wrong{name, "a tensor on the operands' GPU is wanted"};
-  if (t->scalar_type() != type) throw Wrong{name, "a tensor of another type is wanted"};
-  if (t->sizes() != at::IntArrayRef(shape, kN)) throw Wrong{name, "a tensor of another shape is wanted"};
-  if (!t->is_contiguous()) throw Wrong{name, "a contiguous tensor is wanted"};
-  return t->data_ptr();
-}
-
-struct Rows {
-  void *at;
-  int64_t stride, head_stride;
-};
-// a tensor of three dimensions whose last one is contiguous
-Rows rows_of(const Tensor &t, const char *name, at::ScalarType type, int64_t a, int64_t b, int64_t c, int device) {
-  if (!t.is_cuda() || t.get_device() != device) throw Wrong{name, "a tensor on the operands' GPU is wanted"};
-  if (t.scalar_type() != type) throw Wrong{name, "a tensor of another type is wanted"};
-  const auto size = t.sizes();
-  if (size.size() != 3 || size[0] != a || size[1] != b || size[2] != c) throw Wrong{name, "a tensor of another shape is wanted"};
-  const auto stride = t.strides();
-  if (stride[2] != 1 && c != 1) throw Wrong{name, "the last dimension has to be contiguous"};
-  return {t.data_ptr(), stride[0], stride[1]};
-}
-
-int32_t int32_of(int64_t n, const char *name) {
-  if (n > INT32_MAX || n < INT32_MIN) throw Wrong{name, "too large"};
-  return (int32_t)n;
-}
-int64_t number(PyObject *o) {
-  const long long n = PyLong_AsLongLong(o);
-  if (n == -1 && PyErr_Occurred()) throw python_error();
-  return n;
-}
-double real(PyObject *o) {
-  const double x = PyFloat_AsDouble(o);
-  if (x == -1 && PyErr_Occurred()) throw python_error();
-  return x;
-}
-int32_t bound(PyObject *o, int64_t otherwise, const char *name) { return int32_of(o == Py_None ? otherwise : number(o), name); }
-
-const hf_kv_cache *cache_of(PyObject *o) {
-  if (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof(hf_kv_cache)) throw Wrong{"cache", "an hf_kv_cache in bytes is wanted"};
-  return reinterpret_cast<const hf_kv_cache *>(PyBytes_AS_STRING(o));
-}
-// the buffers of a cache, which have to be where the operands are
-void same_gpu(PyObject *keys, PyObject *values, int device) {
-  for (PyObject *o : {keys, values})
-    if (const Tensor &t = wanted(o, "cache"); !t.is_cuda() || t.get_device() != device) throw Wrong{"cache", "a cache on the operands' GPU is wanted"};
-}
-// The cache's operators have no backward: where torch would take a gradient they refuse, rather than lose it in silence.
-void without_gradient(std::initializer_list<std::pair<const char *, const Tensor *>> tensors) {
-  if (!c10::GradMode::is_enabled()) return;
-  for (const auto &[name, t] : tensors)
-    if (t && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
-}
-// what a call has written to, for whoever saved it for a backward pass
-void written(std::initializer_list<const Tensor *> tensors) {
-  for (const Tensor *t : tensors)
-    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
-}
-at::ScalarType type_of(const hf_kv_cache &c) { return c.dtype == HF_BF16 ? at::kBFloat16 : at::kHalf; }
-void *stream_of(PyObject *o) {
-  void *s = PyLong_AsVoidPtr(o);
-  if (!s && PyErr_Occurred()) throw python_error();
-  return s;
-}
-
-// what HfError says; always null
-PyObject *failed(int code, const char *call) {
-  PyObject *e = PyObject_CallFunction(g_error, "is", code, call);
-  if (e) {
-    PyErr_SetObject(g_error, e);
-    Py_DECREF(e);
-  }
-  return nullptr;
-}
-PyObject *wrap(Tensor t) { return THPVariable_Wrap(std::move(t)); }
-PyObject *again(PyObject *o) {
-  Py_INCREF(o);
-  return o;
-}
-
-template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, const F &f) {
-  HANDLE_TH_ERRORS
-  if (n != want) {
-    PyErr_Format(PyExc_TypeError, "%zd arguments are wanted", want);
-    return nullptr;
-  }
-  try {
-    return f();
-  } catch (const Wrong &w) {
-    PyErr_Format(PyExc_ValueError, "%s: %s", w.name, w.what);
-    return nullptr;
-  }
-  END_HANDLE_TH_ERRORS
-}
 
 // (cache, its keys, its values, stream, k, v, slots, positions, cos, sin, q, q_out, interleaved) -> q_out
 PyObject *append(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
@@ -249,35 +119,11 @@ PyObject *attend(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
   });
 }
 
-hf_logits logits_of(const Tensor &logits, const Tensor *targets, PyObject *temperature) {
-  if (!logits.is_cuda() || logits.dim() != 2) throw Wrong{"logits", "[rows, vocab] on the GPU is wanted"};
-  hf_logits a = {};
-  switch (logits.scalar_type()) {
-  case at::kBFloat16: a.dtype = HF_BF16; break;
-  case at::kHalf: a.dtype = HF_F16; break;
-  case at::kFloat: a.dtype = HF_F32; break;
-  default: throw Wrong{"logits", "bfloat16, float16 or float32 is wanted"};
-  }
-  if (logits.stride(1) != 1 && logits.size(1) != 1) throw Wrong{"logits", "the last dimension has to be contiguous"};
-  a.logits = logits.data_ptr();
-  a.rows = logits.size(0), a.row_stride = logits.stride(0), a.vocab = int32_of(logits.size(1), "logits");
-  a.target_bytes = 8;
-  if (targets) {
-    const bool narrow = targets->scalar_type() == at::kInt;
-    a.targets = whole(targets, "targets", narrow ? at::kInt : at::kLong, {a.rows}, logits.get_device());
-    a.target_bytes = narrow ? 4 : 8;
-  }
-  const double t = real(temperature);
-  if (!(t > 0)) throw Wrong{"temperature", "it has to be positive"};
-  a.inv_temperature = (float)(1 / t);
-  return a;
-}
-
 // (stream, logits, targets, temperature, top, apart) -> (logprob, entropy, lse and norm in one, ids, log probabilities, logprob in a tensor of its own if it is wanted apart)
 PyObject *token_logprobs(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
   return guarded(n_args, 6, [&]() -> PyObject * {
     const Tensor &logits = wanted(arg[1], "logits"), *targets = given(arg[2], "targets");
-    const hf_logits a = logits_of(logits, targets, arg[3]);
+    const hf_logits a = logits_of(logits, targets, real(arg[3]));
     const c10::DeviceGuard current(logits.device());
     const int64_t top = number(arg[4]);
     if (top < 0 || top > HF_MAX_TOP) throw Wrong{"top", "0 to HF_MAX_TOP is wanted"};
@@ -311,7 +157,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
 PyObject *token_logprobs_back(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
   return guarded(n_args, 9, [&]() -> PyObject * {
     const Tensor &logits = wanted(arg[1], "logits"), &targets = wanted(arg[2], "targets"), &norm = wanted(arg[3], "norm");
-    const hf_logits a = logits_of(logits, &targets, arg[7]);
+    const hf_logits a = logits_of(logits, &targets, real(arg[7]));
     const c10::DeviceGuard current(logits.device());
     const int device = logits.get_device();
     hf_logprobs_grad g = {};
@@ -332,13 +178,6 @@ PyObject *token_logprobs_back(PyObject *, PyObject *const *arg, Py_ssize_t n_arg
   });
 }
 
-PyObject *set_error(PyObject *, PyObject *type) {
-  Py_XDECREF(g_error);
-  g_error = again(type);
-  Py_RETURN_NONE;
-}
-
-template <typename F> PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 PyMethodDef g_methods[] = {{"append", fast(append), METH_FASTCALL, nullptr},
                            {"attend", fast(attend), METH_FASTCALL, nullptr},
                            {"token_logprobs", fast(token_logprobs), METH_FASTCALL, nullptr},

@@ -1,0 +1,29 @@
+// Launch interface between the C entry points of what surrounds a rollout's steps and their kernels.  Not part of the ABI.
+// Every function expects arguments that its entry point has checked, never allocates or synchronises and returns a hipError_t value (0 = success).
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "hfreshard.h"
+#include "rollout_kernels.hpp" // enqueue_kernel, kMaxWgs
+
+namespace hf {
+
+// workgroups of adjust_logits
+uint64_t adjust_wgs(const hf_adjustment &args);
+int launch_adjust(const hf_adjustment &args, void *stream);
+
+int launch_top_distill(const hf_logits &in, const hf_distillation &args, void *stream);
+int launch_top_distill_back(const hf_logits &in, const hf_distillation_grad &grad, void *stream);
+// workgroups per row of top_distill_back
+uint32_t distill_back_segments(const hf_logits &in);
+
+// elements per access when pages are copied: the widest (8, 4, 2, 1) that divides the head, every stride and address
+size_t fork_workspace(const hf_page_pool &pool, const hf_page_fork &args);
+size_t grow_workspace(const hf_page_pool &pool, const hf_page_grow &args);
+size_t compact_workspace(const hf_page_pool &pool, const hf_page_compact &args);
+int launch_fork(const hf_page_pool &pool, const hf_page_fork &args, int vec, void *stream);
+int launch_grow(const hf_page_pool &pool, const hf_page_grow &args, void *stream);
+int launch_compact(const hf_page_pool &pool, const hf_page_compact &args, int vec, void *stream);
+
+} // namespace hf

@@ -1,22 +1,24 @@
 """The rollout operators for callers that use PyTorch: a paged cache of keys and values that is appended to and attended
-over, and log probabilities of given tokens with their gradient.  torch allocates and hands out pointers and streams; a
-native module (_rollout) checks types and shapes and calls the library, which checks sizes and strides; all work runs in its HIP kernels
+over, its pages (forked, grown, compacted), log probabilities of given tokens with their gradient, logits adjusted before a token is chosen, and
+distillation from a teacher's top tokens.  torch allocates and hands out pointers and streams; two
+native modules (_rollout, _steps) check types and shapes and call the library, which checks sizes and strides; all work runs in its HIP kernels
 on torch's current stream of the tensors' GPU, whichever is current; all tensors of a call are on one.  There is no CPU path.
 """
 from __future__ import annotations
 
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
 from . import binding as B
 
 try:
-    from . import _rollout as _native
+    from . import _rollout as _native, _steps
 except ImportError as e:
     raise ImportError(f"{e}: build it with `python -m paper_2409_19256_amd.build` (there is no fallback path)") from e
 
 _native.set_error(B.HfError)
+_steps.set_error(B.HfError)
 _TYPES = {torch.bfloat16: B.HF_BF16, torch.float16: B.HF_F16}
 _stream_of = torch._C._cuda_getCurrentRawStream
 
@@ -134,3 +136,106 @@ def logprobs(logits: torch.Tensor, targets: torch.Tensor, temperature: float = 1
     """(log probability of targets, entropy) of every row, differentiable with respect to the logits."""
     _need(targets is not None, "targets: a tensor is wanted (entropy alone: token_logprobs)")
     return _Logprobs.apply(logits, targets, temperature)
+
+
+def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None,
+                  prompt_lens: Optional[torch.Tensor] = None, *, repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                  presence: Optional[torch.Tensor] = None, bias_ids: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                  allowed: Optional[torch.Tensor] = None, allowed_rows: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Logits [rows, vocab] on their way to a choice of token.  tokens [rows, width] (int32 or int64) are what a row has so far, lens[row] of them (int32), the first
+    prompt_lens[row] its prompt.  A token that is there: x / repetition[row] where x > 0, else x * repetition[row]; n times behind the prompt: less
+    frequency[row] * n + presence[row] (all float32 [rows]).  bias_ids, bias [rows, places] (int32, float32): added to their tokens, of several the last; ids outside the vocabulary
+    are left out.  allowed (int32 [masks, ceil(vocab / 32)], bit j % 32 of word j / 32): tokens whose bit is not set become -inf, by the mask
+    allowed_rows[row] (int32; outside the masks: none) or by the row's own.  out may be the logits, then only what changes is written.  For
+    generation: it takes no gradient, and refuses tensors that require one where torch would take it."""
+    return _steps.adjust(_stream_of(_device_of(logits)), logits, tokens, lens, prompt_lens, repetition, frequency, presence, bias_ids, bias, allowed, allowed_rows, out)
+
+
+class Distilled:
+    """What top_distill gives: loss [rows], and norm [rows, 2] and slopes [rows, places + 1] for top_distill_back."""
+    __slots__ = ("loss", "norm", "slopes")
+
+    def __init__(self, loss, norm, slopes):
+        self.loss, self.norm, self.slopes = loss, norm, slopes
+
+    def __iter__(self):
+        return iter((self.loss, self.norm, self.slopes))
+
+
+def top_distill(logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, temperature: float = 1.0, reverse: float = 0.0,
+                rest: bool = True) -> Distilled:
+    """How far every row of logits [rows, vocab] over the temperature is from a teacher known by log probabilities of some tokens, top_ids and top_logprobs
+    [rows, places] (int32, float32; what token_logprobs(top=...) gives): (1 - reverse) KL(teacher || student) + reverse KL(student || teacher) over these
+    tokens and, with rest, all others as one more.  Ids outside the vocabulary and log probabilities of -inf name nothing; rows without
+    a name are left out (loss 0).  Not differentiable by itself: see distill."""
+    return Distilled(*_steps.distill(_stream_of(_device_of(logits)), logits, top_ids, top_logprobs, temperature, reverse, rest))
+
+
+def top_distill_back(logits: torch.Tensor, top_ids: torch.Tensor, norm: torch.Tensor, slopes: torch.Tensor, grad_loss: torch.Tensor, temperature: float = 1.0,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum(grad_loss * loss) with respect to the logits; out may be the logits."""
+    return _steps.distill_back(_stream_of(_device_of(logits)), logits, top_ids, norm, slopes, grad_loss, temperature, out)
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, top_ids, top_logprobs, temperature, reverse, rest):
+        loss, norm, slopes = _steps.distill(_stream_of(_device_of(logits)), logits, top_ids, top_logprobs, temperature, reverse, rest)
+        ctx.save_for_backward(logits, top_ids, norm, slopes)
+        ctx.temperature = temperature
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        logits, top_ids, norm, slopes = ctx.saved_tensors
+        # a gradient that was broadcast from a sum has stride 0
+        return top_distill_back(logits, top_ids, norm, slopes, grad_loss.contiguous(), ctx.temperature), None, None, None, None, None
+
+
+def distill(logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, temperature: float = 1.0, reverse: float = 0.0,
+            rest: bool = True) -> torch.Tensor:
+    """top_distill's loss of every row, differentiable with respect to the logits.  The teacher takes no gradient."""
+    _need(not (torch.is_grad_enabled() and isinstance(top_logprobs, torch.Tensor) and top_logprobs.requires_grad),
+          "top_logprobs: no gradient is taken to the teacher: detach them")
+    return _Distill.apply(logits, top_ids, top_logprobs, temperature, reverse, rest)
+
+
+class PagePool:
+    """The pages of a model's caches (KvCache, one per layer, all alike): sequences are tables of page numbers (int32 [rows, width], as KvCache.attend takes
+    them) with lengths in tokens (int32 [rows]), and refs (int32 [pages]) counts the rows that name a page; one with 0 is free.  Full pages may be shared, one that is not full
+    belongs to one row.  All calls run on the GPU without a trip to the host; what they return is new unless given (refs_out may be refs)."""
+
+    def __init__(self, caches: Sequence[KvCache]):
+        _need(len(caches) > 0 and all(isinstance(c, KvCache) for c in caches), "at least one KvCache is wanted")
+        first = caches[0].k
+        _need(all(c.k.shape == first.shape and c.k.stride() == first.stride() and c.k.dtype == first.dtype and c.k.device == first.device for c in caches),
+              "the caches of a pool have to be alike")
+        self.caches = list(caches)
+        self._c, self._tensors = b"".join(c._c for c in caches), tuple(t for c in caches for t in (c.k, c.v))
+
+    def refs(self) -> torch.Tensor:
+        """The reference counts of a pool that nothing is in."""
+        k = self.caches[0].k
+        return torch.zeros(k.shape[0], dtype=torch.int32, device=k.device)
+
+    def fork(self, tables: torch.Tensor, lens: torch.Tensor, parents: torch.Tensor, refs: torch.Tensor, tables_out: Optional[torch.Tensor] = None,
+             lens_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        """Row r goes on where row parents[r] (int32; outside the rows: empty) stands; rows that nobody continues give their pages back.  Full pages are
+        shared; of a page that is not full the first row that continues it has it and the others take copies.  A row for which no page is left comes out empty.  Returns (tables, lens, refs)."""
+        return _steps.fork(self._c, self._tensors, _stream_of(_device_of(tables)), tables, lens, parents, refs, tables_out, lens_out, refs_out, workspace)
+
+    def grow(self, tables: torch.Tensor, lens: torch.Tensor, counts: torch.Tensor, refs: torch.Tensor, most: int = 1, tables_out: Optional[torch.Tensor] = None,
+             lens_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None):
+        """Room for counts[row] more tokens (int32, cut to 0 .. most) in every row.  slots [rows, most] (int64) are their places for KvCache.append, -1 where
+        there is none.  A row that does not fit the table or for which no pages are left stays as it is.  tables_out may be tables, lens_out lens.  Returns
+        (tables, lens, slots, refs)."""
+        return _steps.grow(self._c, self._tensors, _stream_of(_device_of(tables)), tables, lens, counts, refs, most, tables_out, lens_out, slots, refs_out, workspace)
+
+    def compact(self, refs: torch.Tensor, tables: Sequence[torch.Tensor] = (), tables_out: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                refs_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        """Moves pages so that the n in use are the first n.  Up to four tables (any shape) have their entries replaced.  Returns (tables, refs, places, n): where
+        every page is now (int32, -1: free), and n (int32, no dimension).  tables_out may be tables."""
+        return _steps.compact(self._c, self._tensors, _stream_of(_device_of(refs)), refs, tuple(tables), tuple(tables_out) if tables_out is not None else (None,) * len(tables),
+                              refs_out, workspace)
