@@ -3,8 +3,13 @@
 //   seen: x > 0 ? x / r : x r;   n times in the answer: - f n - p;   bias: + b;   ruled out: -inf
 //
 // Every logit is read once and written once, so HBM is the bound.  A workgroup takes a piece of a row: it asks for its logits, counts the row's tokens that
-// fall into the piece in shared memory while they are on their way, keeps them there, changes those that were counted or have a bias (each by one lane: the one that
-// counted first, or whose bias is the last), and writes the piece.  In place nothing is moved but what changes.
+// fall into the piece in shared memory while they are on their way, lays them there, changes those that were counted or have a bias, each by one lane (whose bias
+// is the token's last, or who is first to take the count away), and writes the piece.  The work beside the copy goes by the tokens and biases, not by the logits: a look at
+// every logit's count took more than HBM leaves room for.  In place and without a mask nothing is moved but what changes.
+//
+// us, out of place, beside the copy alone by the same workgroups: 1024 x 32000 bf16, 900 tokens a row, half of the rows masked 24.2 beside 22.0; 1024 x 128256 f32, 2800 tokens and 64 biases a row,
+// half masked 208 beside 170-189 (5.1 TB/s); 64 x 32000 bf16 4.8, one workgroup after another's data (lengths, tokens, counts, logits).  Pieces of 4096 / 8192 / 16384 (256 / 512 / 1024 lanes)
+// take 33 / 27 / 26 and 254 / 210 / 245, so do 512 lanes for 4096 (35, 250) or 1024 for 8192 (35, 221).
 #include <hip/hip_runtime.h>
 
 #include "logit_rows.hpp"
@@ -14,146 +19,179 @@ namespace hf {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kChunk = 4096;                 // logits of a piece
-constexpr uint32_t kPrompt = 0x80000000u;    // a count's bit: the token stands in the prompt
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 512, kWave = 64;
+constexpr int kChunk = 8192; // logits of a piece
+constexpr int kHeld = 8;     // of a row's tokens that a lane keeps in registers
 
 struct Row { // what one row's elements are changed by
   float rep, freq, pres;
-  const float *bias;
-  const uint8_t *allowed; // null: all
 };
-
-__device__ __forceinline__ float penalised(float x, uint32_t count, const Row &row) {
-  if (count == 0) return x;
-  x = x > 0 ? x / row.rep : x * row.rep;
-  const uint32_t n = count & ~kPrompt;
+// n: times in the answer, and whether the token is there at all
+__device__ __forceinline__ float penalised(float x, uint32_t n, bool seen, const Row &row) {
+  if (seen) x = x > 0 ? x / row.rep : x * row.rep;
   return n ? x - row.freq * (float)n - row.pres : x;
 }
 
+// How often tokens of the piece stand in the row: a number each, whose highest bit says that the token stands in the prompt.  16 bits are enough for
+// rows of fewer than 2^15 tokens, two numbers to a word; others take a word each.
+template <bool kWide> struct Counts {
+  static constexpr int kWords = kWide ? kChunk : kChunk / 2;
+  static constexpr uint32_t kPrompt = kWide ? 0x80000000u : 0x8000u;
+  static __device__ __forceinline__ void add(uint32_t *words, int at, bool prompt) {
+    const int shift = kWide ? 0 : at % 2 * 16;
+    uint32_t *word = words + (kWide ? at : at / 2);
+    if (prompt) atomicOr(word, kPrompt << shift);
+    else atomicAdd(word, 1u << shift);
+  }
+  // the number, which is 0 for whoever asks next
+  static __device__ __forceinline__ uint32_t take(uint32_t *words, int at) {
+    if (kWide) return atomicExch(words + at, 0u);
+    const int shift = at % 2 * 16;
+    return atomicAnd(words + at / 2, ~(0xFFFFu << shift)) >> shift & 0xFFFFu;
+  }
+};
+
 // the bits of vector `v` of a row: 8 elements or 4
-template <typename T> __device__ __forceinline__ uint32_t allowed_of(const uint8_t *allowed, int v) {
+template <typename T> __device__ __forceinline__ uint32_t bits_of(const uint8_t *allowed, int v) {
   return kVec<T> == 8 ? allowed[v] : allowed[v / 2] >> (v % 2 * 4) & 15u;
 }
 
-template <typename T, bool kTables, bool kInPlace> __global__ __launch_bounds__(kThreads) void adjust_logits(hf_adjustment a, uint32_t pieces) {
+template <typename T, typename Token, bool kTables, bool kWide> __global__ __launch_bounds__(kThreads) void adjust_logits(hf_adjustment a, uint32_t pieces) {
   constexpr int kV = kVec<T>, kPer = kChunk / kV / kThreads; // vectors of a lane
-  constexpr uint32_t kAll = (1u << kV) - 1;
   typedef typename Vector<T>::type V;
-  __shared__ uint32_t count[kTables ? kChunk : 1], bias_at[kTables ? kChunk : 1];
-  __shared__ __attribute__((aligned(16))) T tile[kTables && !kInPlace ? kChunk : 1];
-  __shared__ uint16_t touched[kTables ? kChunk : 1];
-  __shared__ uint32_t n_touched;
+  typedef Counts<kWide> C;
+  __shared__ __attribute__((aligned(16))) uint32_t count[kTables ? C::kWords : 1];
+  __shared__ __attribute__((aligned(16))) T tile[kTables ? kChunk : 1];
   const int t = threadIdx.x;
-  const int64_t r = blockIdx.x / pieces;
-  const int begin = blockIdx.x % pieces * kChunk, size = min(kChunk, a.vocab - begin), n_vec = size / kV; // whole vectors; the others are the row's last elements
+  // the pieces of a row on one XCD (workgroups go round them by eights), whose L2 then reads the row's tokens once: 1024 x 32000 bf16 24.2 us for 27.7
+  const uint32_t turned = (uint32_t)(a.rows / 8) * 8 * pieces, b = blockIdx.x;
+  const int64_t r = b < turned ? (int64_t)(b / 8 / pieces) * 8 + b % 8 : b / pieces;
+  const int begin = (b < turned ? b / 8 % pieces : b % pieces) * kChunk, size = min(kChunk, a.vocab - begin), n_vec = size / kV; // whole vectors; the others are the row's last elements
   const T *from = static_cast<const T *>(a.logits) + r * a.row_stride + begin;
   T *to = static_cast<T *>(a.out) + r * a.out_stride + begin;
-  Row row = {a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f, a.presence ? a.presence[r] : 0.f, nullptr, nullptr};
-  if (a.n_bias) row.bias = a.bias + r * a.n_bias;
+  const uint8_t *allowed = nullptr; // all
   if (a.allowed) {
     const int64_t g = a.allowed_rows ? a.allowed_rows[r] : r;
-    if (g >= 0 && g < a.n_allowed) row.allowed = reinterpret_cast<const uint8_t *>(a.allowed + g * a.allowed_stride) + begin / 8;
+    if (g >= 0 && g < a.n_allowed) allowed = reinterpret_cast<const uint8_t *>(a.allowed + g * a.allowed_stride) + begin / 8;
   }
-  const auto open = [&](int i) { return !row.allowed || row.allowed[i / 8] >> i % 8 & 1; };
+  const bool sparse = from == to && !allowed; // nothing is moved but what changes
+  if (!kTables && sparse) return;
+  const int n_last = sparse ? 0 : min(kV, size - n_vec * kV); // elements past the whole vectors, a lane each
 
   V v[kPer];
-  if constexpr (!kInPlace) {
+  uint32_t bits[kPer];
+  if (!sparse) {
 #pragma unroll
     for (int k = 0; k < kPer; ++k)
       if (t + k * kThreads < n_vec) v[k] = load_once(from + (t + k * kThreads) * kV);
+    if (allowed) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (t + k * kThreads < n_vec) bits[k] = bits_of<T>(allowed, t + k * kThreads);
+    }
   }
   if constexpr (kTables) {
-    for (int i = t; i < kChunk; i += kThreads) count[i] = bias_at[i] = 0;
-    if (t == 0) n_touched = 0;
+    const int n = a.tokens ? min(max(a.lens[r], 0), a.width) : 0, prompt = a.prompt_lens ? a.prompt_lens[r] : 0;
+    const Row row = {a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f, a.presence ? a.presence[r] : 0.f};
+    const Token *tokens = static_cast<const Token *>(a.tokens) + r * a.tokens_stride;
+    Token held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (t + k * kThreads < n) held[k] = tokens[t + k * kThreads];
+    const int32_t *ids = a.bias_ids + r * a.n_bias;
+    int id = t < a.n_bias ? ids[t] : -1;
+    float bias = t < a.n_bias ? a.bias[r * a.n_bias + t] : 0.f;
+    for (int i = t; i < C::kWords / 4; i += kThreads) reinterpret_cast<u32x4 *>(count)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
-    if (a.tokens) {
-      const int n = min(max(a.lens[r], 0), a.width), prompt = a.prompt_lens ? a.prompt_lens[r] : 0;
-      const auto add = [&](int64_t token, int i) {
-        const int64_t at = token - begin;
-        if (at < 0 || at >= size) return;
-        const uint32_t old = i < prompt ? atomicOr(&count[at], kPrompt) : atomicAdd(&count[at], 1u);
-        if (old == 0) touched[atomicAdd(&n_touched, 1u)] = at;
-      };
-      if (a.token_bytes == 8) {
-        const int64_t *tokens = static_cast<const int64_t *>(a.tokens) + r * a.tokens_stride;
-        for (int i = t; i < n; i += kThreads) add(tokens[i], i);
-      } else {
-        const int32_t *tokens = static_cast<const int32_t *>(a.tokens) + r * a.tokens_stride;
-        for (int i = t; i < n; i += kThreads) add(tokens[i], i);
-      }
-    }
-    for (int j = t; j < a.n_bias; j += kThreads) {
-      const int64_t at = (int64_t)a.bias_ids[r * a.n_bias + j] - begin;
-      if (at >= 0 && at < size) atomicMax(&bias_at[at], j + 1u);
-    }
-    if constexpr (!kInPlace) {
+    // f(place in the piece, place in the row) for the tokens of the piece
+    const auto each = [&](const auto &f) {
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k)
+        if (t + k * kThreads < n)
+          if (const int64_t at = (int64_t)held[k] - begin; at >= 0 && at < size) f((int)at, t + k * kThreads);
+      for (int i = t + kHeld * kThreads; i < n; i += kThreads)
+        if (const int64_t at = (int64_t)tokens[i] - begin; at >= 0 && at < size) f((int)at, i);
+    };
+    each([&](int at, int i) { C::add(count, at, i < prompt); });
+    if (!sparse) {
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
         if (t + k * kThreads < n_vec) *reinterpret_cast<V *>(tile + (t + k * kThreads) * kV) = v[k];
-      if (const int i = n_vec * kV + t; t < kV && i < size) tile[i] = from[i];
+      if (t < n_last) tile[n_vec * kV + t] = from[n_vec * kV + t];
     }
     __syncthreads();
-    const auto change = [&](int i, float bias) {
-      if constexpr (kInPlace) {
-        if (open(i)) to[i] = (T)(penalised((float)to[i], count[i], row) + bias);
-      } else {
-        tile[i] = (T)(penalised((float)tile[i], count[i], row) + bias);
-      }
+    const auto change = [&](int i, uint32_t counted, float add) {
+      T *x = sparse ? to + i : tile + i;
+      *x = (T)(penalised((float)*x, counted & ~C::kPrompt, counted != 0, row) + add);
     };
-    for (uint32_t k = t; k < n_touched; k += kThreads)
-      if (const int i = touched[k]; bias_at[i] == 0) change(i, 0.f);
-    for (int j = t; j < a.n_bias; j += kThreads) {
-      const int64_t at = (int64_t)a.bias_ids[r * a.n_bias + j] - begin;
-      if (at >= 0 && at < size && bias_at[at] == j + 1u) change(at, row.bias[j]);
+    if (a.n_bias) {
+      for (int j0 = t / kWave * kWave; j0 < a.n_bias; j0 += kThreads) { // a wavefront's places of the list
+        if (j0 >= kThreads) {
+          const int j = j0 + t % kWave;
+          id = j < a.n_bias ? ids[j] : -1;
+          bias = j < a.n_bias ? a.bias[r * a.n_bias + j] : 0.f;
+        }
+        const bool here = id >= begin && id - begin < size;
+        uint64_t holding = __ballot(here); // the lanes whose biases hold: none behind is of the same token
+        for (uint64_t left = holding; left; left &= left - 1) {
+          const int l = __builtin_ctzll(left);
+          if (__ballot(id == __builtin_amdgcn_readlane(id, l)) >> l > 1) holding &= ~(1ull << l);
+        }
+        for (int k0 = j0 + kWave; holding && k0 < a.n_bias; k0 += kWave) {
+          const int other = k0 + t % kWave < a.n_bias ? ids[k0 + t % kWave] : -1;
+          for (uint64_t left = holding; left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            if (__ballot(other == __builtin_amdgcn_readlane(id, l))) holding &= ~(1ull << l);
+          }
+        }
+        if (holding >> t % kWave & 1) change(id - begin, C::take(count, id - begin), bias);
+      }
+      __syncthreads();
     }
-    if constexpr (!kInPlace) __syncthreads();
+    each([&](int at, int) {
+      if (const uint32_t counted = C::take(count, at)) change(at, counted, 0.f);
+    });
+    if (sparse) return;
+    __syncthreads();
   }
-  if constexpr (kInPlace) {
-    if (!row.allowed) return;
-    for (int k = t; k < n_vec; k += kThreads) {
-      const uint32_t bits = allowed_of<T>(row.allowed, k);
-      if (bits == 0) {
-        V ruled;
 #pragma unroll
-        for (int e = 0; e < kV; ++e) ruled[e] = (T)-INFINITY;
-        *reinterpret_cast<typename Vector<T>::any *>(to + k * kV) = ruled;
-      } else if (bits != kAll) {
+  for (int k = 0; k < kPer; ++k) {
+    const int at = t + k * kThreads;
+    if (at >= n_vec) break;
+    if constexpr (kTables) v[k] = *reinterpret_cast<const V *>(tile + at * kV);
+    if (allowed) {
 #pragma unroll
-        for (int e = 0; e < kV; ++e)
-          if (!(bits >> e & 1)) to[k * kV + e] = (T)-INFINITY;
-      }
+      for (int e = 0; e < kV; ++e) v[k][e] = bits[k] >> e & 1 ? v[k][e] : (T)-INFINITY;
     }
-    if (const int i = n_vec * kV + t; t < kV && i < size && !open(i)) to[i] = (T)-INFINITY;
-  } else {
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int at = t + k * kThreads;
-      if (at >= n_vec) break;
-      if constexpr (kTables) v[k] = *reinterpret_cast<const V *>(tile + at * kV);
-      if (row.allowed) {
-        const uint32_t bits = allowed_of<T>(row.allowed, at);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) v[k][e] = bits >> e & 1 ? v[k][e] : (T)-INFINITY;
-      }
-      *reinterpret_cast<typename Vector<T>::any *>(to + at * kV) = v[k];
-    }
-    if (const int i = n_vec * kV + t; t < kV && i < size) to[i] = open(i) ? (kTables ? tile[i] : from[i]) : (T)-INFINITY;
+    store_once(to + at * kV, v[k]);
+  }
+  if (t < n_last) {
+    const int i = n_vec * kV + t;
+    const T x = kTables ? tile[i] : from[i];
+    to[i] = !allowed || allowed[i / 8] >> i % 8 & 1 ? x : (T)-INFINITY;
   }
 }
 
+template <typename T, typename Token, bool kWide> hipError_t launch_tables(const hf_adjustment &a, const dim3 &grid, uint32_t pieces, hipStream_t st) {
+  return enqueue_kernel(adjust_logits<T, Token, true, kWide>, grid, kThreads, st, a, pieces);
+}
 template <typename T> hipError_t launch(const hf_adjustment &a, hipStream_t st) {
   const uint32_t pieces = (a.vocab + kChunk - 1) / kChunk;
   const dim3 grid((uint32_t)(a.rows * pieces));
-  const bool tables = (a.tokens && a.width) || a.n_bias, in_place = a.logits == a.out;
-  if (in_place && !tables && !a.allowed) return hipSuccess;
-  const auto kernel = tables ? in_place ? adjust_logits<T, true, true> : adjust_logits<T, true, false> : in_place ? adjust_logits<T, false, true> : adjust_logits<T, false, false>;
-  return enqueue_kernel(kernel, grid, kThreads, st, a, pieces);
+  const bool text = a.tokens && a.width, wide = text && a.width >= 1 << 15;
+  if (text && a.token_bytes == 8) return wide ? launch_tables<T, int64_t, true>(a, grid, pieces, st) : launch_tables<T, int64_t, false>(a, grid, pieces, st);
+  if (text || a.n_bias) return wide ? launch_tables<T, int32_t, true>(a, grid, pieces, st) : launch_tables<T, int32_t, false>(a, grid, pieces, st);
+  if (a.logits == a.out && !a.allowed) return hipSuccess;
+  return enqueue_kernel(adjust_logits<T, int32_t, false, false>, grid, kThreads, st, a, pieces);
 }
 
 } // namespace
 
-uint64_t adjust_wgs(const hf_adjustment &a) { return (uint64_t)a.rows * ((a.vocab + kChunk - 1) / kChunk); }
+uint64_t adjust_wgs(const hf_adjustment &a) {
+  return (uint64_t)a.rows * ((a.vocab + kChunk - 1) / kChunk);
+}
 
 int launch_adjust(const hf_adjustment &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
