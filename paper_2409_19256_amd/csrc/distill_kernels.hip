@@ -303,11 +303,11 @@ template <typename T, int kThreads, int kPlaces, bool kOnce> __global__ __launch
 }
 
 constexpr int kBackThreads = 256;
-constexpr int kBackVectors = 4; // a lane's vectors
+template <typename T> constexpr int kBackVectors = sizeof(T) == 4 ? 2 : 4; // a lane's vectors
 
 // A workgroup takes one of `segments` pieces of a row.
 template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distill_back(Logits in, hf_distillation_grad g, uint32_t segments) {
-  constexpr int kV = kVec<T>, kPiece = kBackThreads * kBackVectors * kV;
+  constexpr int kV = kVec<T>, kVectors = kBackVectors<T>, kPiece = kBackThreads * kVectors * kV;
   typedef typename Vector<T>::type V;
   __shared__ uint32_t named[kPiece / 32];
   __shared__ T value[kPiece]; // of the named elements alone
@@ -322,9 +322,9 @@ template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distil
     return;
   }
   const T *row = static_cast<const T *>(in.data) + r * in.row_stride + begin;
-  V v[kBackVectors];
+  V v[kVectors];
 #pragma unroll
-  for (int k = 0; k < kBackVectors; ++k)
+  for (int k = 0; k < kVectors; ++k)
     if (t + k * kBackThreads < n_vec) v[k] = load_once(row + (t + k * kBackThreads) * kV);
   const float scale = g.grad_loss[r], *slopes = g.slopes + r * (g.n + 1);
   for (int i = t; i < kPiece / 32; i += kBackThreads) named[i] = 0;
@@ -343,7 +343,7 @@ template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distil
   };
   const uint8_t *bytes = reinterpret_cast<const uint8_t *>(named);
 #pragma unroll
-  for (int k = 0; k < kBackVectors; ++k) {
+  for (int k = 0; k < kVectors; ++k) {
     const int i = t + k * kBackThreads;
     if (i >= n_vec) break;
     const uint32_t bits = kV == 8 ? bytes[i] : bytes[i / 2] >> (i % 2 * 4) & 15;
@@ -383,7 +383,7 @@ template <typename T> hipError_t launch(const hf_logits &in, const hf_distillati
 } // namespace
 
 uint32_t distill_back_segments(const hf_logits &in) {
-  const uint32_t piece = kBackThreads * kBackVectors * (in.dtype == HF_F32 ? kVec<float> : kVec<__bf16>);
+  const uint32_t piece = kBackThreads * (in.dtype == HF_F32 ? kBackVectors<float> * kVec<float> : kBackVectors<__bf16> * kVec<__bf16>);
   return (in.vocab + piece - 1) / piece;
 }
 

@@ -82,29 +82,47 @@ template <> struct Access<8> { typedef uint32_t type __attribute__((ext_vector_t
 template <> struct Access<4> { typedef uint32_t type; };
 template <> struct Access<2> { typedef uint16_t type; };
 
-constexpr int kInFlight = 4;
+constexpr int kInFlight = 8;
 
-// Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.
-template <int kVecBytes> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, int64_t part) {
+// Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.  kOnce: read past the caches.
+template <int kVecBytes, bool kOnce> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, uint32_t part) {
   typedef typename Access<kVecBytes>::type V;
   const uint32_t outer = s.growing == 0 ? tokens : s.outer, middle = s.growing == 1 ? tokens : s.middle, inner = s.growing == 2 ? s.inner * tokens : s.inner;
-  const uint64_t n = (uint64_t)outer * middle * inner;
+  const uint32_t n = outer * middle * inner; // (fits: a page has fewer than 2^31 elements)
   V *base = static_cast<V *>(buffer);
-  uint64_t at = part * (kThreads * kInFlight) + threadIdx.x;
+  uint32_t at = part * (kThreads * kInFlight) + threadIdx.x;
   int64_t off[kInFlight];
   V v[kInFlight];
 #pragma unroll
   for (int k = 0; k < kInFlight; ++k, at += kThreads) {
     if (at >= n) break;
-    const uint32_t run = (uint32_t)at / inner, x = (uint32_t)at % inner;
-    off[k] = run / middle * s.outer_stride + run % middle * s.middle_stride + x;
-    v[k] = base[src * s.page + off[k]];
+    const uint32_t run = at / inner, x = at % inner;
+    off[k] = s.growing == 1 ? run / middle * s.outer_stride + run % middle * s.middle_stride + x : run * s.outer_stride + x;
+    const V *from = base + (src * s.page + off[k]);
+    v[k] = kOnce ? __builtin_nontemporal_load(from) : *from;
   }
   at = part * (kThreads * kInFlight) + threadIdx.x;
 #pragma unroll
   for (int k = 0; k < kInFlight; ++k, at += kThreads) {
     if (at >= n) break;
-    base[dst * s.page + off[k]] = v[k];
+    __builtin_nontemporal_store(v[k], base + (dst * s.page + off[k]));
+  }
+}
+
+// What moves: the first `tokens` tokens of a page, to another one.
+struct Move {
+  int32_t from, tokens;
+};
+// Moves dealt out by parts of a page: f(move, buffer, part) for every `wgs`-th, from `wg` on
+template <typename F> __device__ __forceinline__ void each_part(int64_t moves, uint32_t buffers, uint32_t parts, uint32_t wg, uint32_t wgs, const F &f) {
+  const uint32_t per = buffers * parts, step = wgs / per, more = wgs % per;
+  int64_t k = wg / per;
+  for (uint32_t i = wg % per; k < moves; k += step, i += more) {
+    if (i >= per) {
+      i -= per;
+      if (++k >= moves) break;
+    }
+    f(k, i / parts, i % parts);
   }
 }
 
@@ -120,7 +138,7 @@ struct Fork {
   int64_t *free_sums, *want_sums; // per tile of pages, of rows
   int32_t *free_list;        // [rows_out]
   int32_t *want;             // [rows_out] which free page a row wants; -1 none
-  int32_t *wanting;          // [rows_out] the rows that want one
+  Move *moves;               // [rows_out] what goes into those that are wanted
   int64_t *totals;           // free pages, wanted pages
   int32_t page_tiles, row_tiles;
   int64_t page_tile, row_tile;
@@ -199,42 +217,115 @@ __global__ __launch_bounds__(kThreads) void fork_lists(Fork f) {
       const bool wants = p >= 0 && f.first[p] != r;
       const int64_t at = base + sum_before(wants, shared, &all);
       if (r < end) f.want[r] = wants ? (int32_t)at : -1;
-      if (wants) f.wanting[at] = (int32_t)r;
+      if (wants) f.moves[at] = {p, (int32_t)(len_of(f.from, parent_of(f, r)) & ((1 << f.from.shift) - 1))};
       base += all;
     }
     if (tile == f.row_tiles - 1 && threadIdx.x == 0) f.totals[1] = base;
   }
 }
-template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, int32_t row_wgs, int32_t parts) {
+// what a place of a new row's table holds; `refs`: the counts, in memory or shared
+__device__ __forceinline__ int32_t forked(const Fork &f, int32_t *refs, int64_t parent, int64_t n, int64_t k, bool lost, int32_t fresh) {
+  int32_t p = k < n ? page_at(f.from, parent, k) : -1;
+  if (lost) {
+    if (p >= 0 && k < n - 1) atomicAdd(&refs[p], -1);
+    return -1;
+  }
+  if (fresh >= 0 && k == n - 1) refs[p = fresh] = 1;
+  return p;
+}
+__device__ __forceinline__ void fork_rows(const Fork &f, int64_t wave, int64_t waves) {
   const int64_t free = f.totals[0];
-  if ((int)blockIdx.x < row_wgs) { // a wavefront to a row
-    const int lane = threadIdx.x % kWave;
-    for (int64_t r = blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave; r < f.rows_out; r += (int64_t)row_wgs * kWaves) {
-      const int64_t parent = parent_of(f, r), len = parent < 0 ? 0 : len_of(f.from, parent), n = pages_of(f.from, len);
-      const int32_t want = f.want[r];
-      const bool lost = want >= free;
-      const int32_t fresh = want >= 0 && !lost ? f.free_list[want] : -1;
-      for (int64_t k = lane; k < f.from.width; k += kWave) {
-        int32_t p = k < n ? page_at(f.from, parent, k) : -1;
-        if (lost) {
-          if (p >= 0 && k < n - 1) atomicAdd(&f.refs_out[p], -1);
-          p = -1;
-        } else if (fresh >= 0 && k == n - 1) {
-          p = fresh;
-          f.refs_out[p] = 1;
-        }
-        f.tables_out[r * f.from.width + k] = p;
+  for (int64_t r = wave; r < f.rows_out; r += waves) {
+    const int64_t parent = parent_of(f, r), len = parent < 0 ? 0 : len_of(f.from, parent), n = pages_of(f.from, len);
+    const int32_t want = f.want[r];
+    const bool lost = want >= free;
+    const int32_t fresh = want >= 0 && !lost ? f.free_list[want] : -1;
+    for (int64_t k = threadIdx.x % kWave; k < f.from.width; k += kWave) f.tables_out[r * f.from.width + k] = forked(f, f.refs_out, parent, n, k, lost, fresh);
+    if (threadIdx.x % kWave == 0) f.lens_out[r] = lost ? 0 : (int32_t)len;
+  }
+}
+// row_wgs: workgroups that write tables, a wavefront to a row; the others copy
+template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, uint32_t row_wgs, uint32_t parts) {
+  if (blockIdx.x < row_wgs) return fork_rows(f, blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave, (int64_t)row_wgs * kWaves);
+  each_part(min(f.totals[0], f.totals[1]), buffers.n, parts, blockIdx.x - row_wgs, gridDim.x - row_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
+    const Move m = f.moves[k];
+    copy_part<kVecBytes, false>(buffers.at[b], shape, m.from, f.free_list[k], m.tokens, part); // (several may copy one page)
+  });
+}
+
+// All of the books by one workgroup, counts in shared memory.
+constexpr int kSoloThreads = 1024, kSoloWaves = kSoloThreads / kWave, kSoloPages = 16384, kSoloRows = 2048;
+// how many of the lanes in front have `is`, and in all; `shared` holds one number a wavefront and may be used again at once
+__device__ __forceinline__ int32_t rank_of(bool is, int32_t *shared, int32_t *all) {
+  const uint64_t mask = __ballot(is);
+  const int wave = threadIdx.x / kWave;
+  if (threadIdx.x % kWave == 0) shared[wave] = __popcll(mask);
+  __syncthreads();
+  int32_t base = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kSoloWaves; ++w) {
+    const int32_t n = shared[w];
+    base += w < wave ? n : 0;
+    total += n;
+  }
+  __syncthreads();
+  *all = total;
+  return base + __popcll(mask & ((1ull << threadIdx.x % kWave) - 1));
+}
+__global__ __launch_bounds__(kSoloThreads) void fork_solo(Fork f) {
+  __shared__ int32_t refs[kSoloPages], first[kSoloPages], lens[kSoloRows], parents[kSoloRows], shared[kSoloWaves];
+  const int t = threadIdx.x, width = f.from.width, pages = f.from.n_pages, part = (1 << f.from.shift) - 1;
+  for (int i = t; i < pages; i += kSoloThreads) refs[i] = f.refs[i], first[i] = INT32_MAX;
+  for (int r = t; r < f.from.rows; r += kSoloThreads) lens[r] = (int32_t)len_of(f.from, r);
+  for (int r = t; r < f.rows_out; r += kSoloThreads) parents[r] = (int32_t)parent_of(f, r);
+  __syncthreads();
+  const auto len_at = [&](int parent) { return parent < 0 ? 0 : lens[parent]; };
+  const auto open_at = [&](int parent) { return len_at(parent) & part ? page_at(f.from, parent, lens[parent] >> f.from.shift) : -1; };
+#pragma unroll 4
+  for (int i = t; i < f.from.rows * width; i += kSoloThreads) {
+    const int r = i / width, k = i % width;
+    if (k < pages_of(f.from, lens[r]))
+      if (const int32_t p = page_at(f.from, r, k); p >= 0) atomicAdd(&refs[p], -1);
+  }
+#pragma unroll 4
+  for (int i = t; i < f.rows_out * width; i += kSoloThreads) {
+    const int r = i / width, k = i % width, parent = parents[r], len = len_at(parent), full = len >> f.from.shift;
+    if (k < pages_of(f.from, len))
+      if (const int32_t p = page_at(f.from, parent, k); p >= 0) {
+        if (k < full) atomicAdd(&refs[p], 1);
+        else atomicMin(&first[p], r);
       }
-      if (lane == 0) f.lens_out[r] = lost ? 0 : (int32_t)len;
-    }
-    return;
   }
-  const int64_t pairs = min(free, f.totals[1]), items = pairs * buffers.n * parts;
-  for (int64_t i = (int64_t)blockIdx.x - row_wgs; i < items; i += gridDim.x - row_wgs) {
-    const int64_t part = i % parts, b = i / parts % buffers.n, k = i / parts / buffers.n;
-    const int64_t parent = parent_of(f, f.wanting[k]);
-    copy_part<kVecBytes>(buffers.at[b], shape, open_page(f, parent), f.free_list[k], len_of(f.from, parent) & ((1 << f.from.shift) - 1), part);
+  __syncthreads();
+  int32_t wanted = 0, free = 0, all;
+  for (int r0 = 0; r0 < f.rows_out; r0 += kSoloThreads) {
+    const int r = r0 + t, p = r < f.rows_out ? open_at(parents[r]) : -1;
+    const bool wants = p >= 0 && first[p] != r;
+    const int32_t at = wanted + rank_of(wants, shared, &all);
+    if (r < f.rows_out) f.want[r] = wants ? at : -1;
+    if (wants) f.moves[at] = {p, len_at(parents[r]) & part};
+    wanted += all;
   }
+  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
+    const int i = i0 + t;
+    const bool kept = i < pages && first[i] != INT32_MAX, is = i < pages && refs[i] == 0 && !kept;
+    const int32_t at = free + rank_of(is, shared, &all);
+    if (is && at < wanted) f.free_list[at] = i;
+    if (kept) ++refs[i];
+    free += all;
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int i = t; i < f.rows_out * width; i += kSoloThreads) {
+    const int r = i / width, k = i % width, parent = parents[r];
+    const int32_t want = f.want[r];
+    const bool lost = want >= free;
+    f.tables_out[i] = forked(f, refs, parent, pages_of(f.from, len_at(parent)), k, lost, want >= 0 && !lost ? f.free_list[want] : -1);
+  }
+  for (int r = t; r < f.rows_out; r += kSoloThreads) f.lens_out[r] = f.want[r] >= free ? 0 : len_at(parents[r]);
+  __syncthreads();
+  for (int i = t; i < pages; i += kSoloThreads) f.refs_out[i] = refs[i];
+  if (t == 0) f.totals[0] = free, f.totals[1] = wanted;
 }
 
 // ---- grow ----------------------------------------------------------------------------------------------------------------
@@ -342,6 +433,75 @@ __global__ __launch_bounds__(kThreads) void grow_apply(Grow g) {
   }
 }
 
+// All of it by one workgroup.
+constexpr int kSoloFresh = 8192; // fresh pages that it can hand out
+__global__ __launch_bounds__(kSoloThreads) void grow_solo(Grow g) {
+  __shared__ int32_t list[kSoloFresh], before[kSoloRows], lens[kSoloRows], counts[kSoloRows], shared[kSoloWaves];
+  const int t = threadIdx.x, width = g.from.width, pages = g.from.n_pages, shift = g.from.shift, page_tokens = 1 << shift;
+  int32_t wanted = 0, free = 0, all;
+  for (int r0 = 0; r0 < g.from.rows; r0 += kSoloThreads) {
+    const int r = r0 + t;
+    int32_t need = 0;
+    if (r < g.from.rows) {
+      const Growth x = growth_of(g, r);
+      need = (int32_t)x.need();
+      lens[r] = (int32_t)x.len, counts[r] = x.fits ? x.count : -1;
+    }
+    int32_t upto = need; // sums over the wavefront, then over the workgroup
+    for (int d = 1; d < kWave; d *= 2) {
+      const int32_t y = __shfl_up(upto, d);
+      if (t % kWave >= d) upto += y;
+    }
+    if (t % kWave == kWave - 1) shared[t / kWave] = upto;
+    __syncthreads();
+    int32_t base = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kSoloWaves; ++w) {
+      base += w < t / kWave ? shared[w] : 0;
+      all += shared[w];
+    }
+    __syncthreads();
+    if (r < g.from.rows) before[r] = wanted + base + upto - need;
+    wanted += all;
+  }
+  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
+    const int i = i0 + t;
+    const int32_t refs = i < pages ? g.refs[i] : 1;
+    const int32_t at = free + rank_of(refs == 0, shared, &all);
+    const bool taken = refs == 0 && at < wanted;
+    if (taken) list[at] = i;
+    if (i < pages && g.refs_out != g.refs) g.refs_out[i] = refs;
+    free += all;
+  }
+  __syncthreads();
+  const auto grows = [&](int r, int32_t &have, int32_t &want) {
+    have = (int32_t)pages_of(g.from, lens[r]), want = (int32_t)pages_of(g.from, lens[r] + (int64_t)max(counts[r], 0));
+    return counts[r] >= 0 && (want == have || before[r] + want - have <= free);
+  };
+  int32_t have, want;
+#pragma unroll 2
+  for (int i = t; i < g.from.rows * g.most; i += kSoloThreads) { // (the tables are read before they are written: they may be the same)
+    const int r = i / g.most, at = lens[r] + i % g.most, k = at >> shift;
+    int64_t slot = -1;
+    if (grows(r, have, want) && i % g.most < counts[r]) {
+      const int64_t p = k < have ? page_at(g.from, r, k) : list[before[r] + k - have];
+      if (p >= 0) slot = (p << shift) + (at & (page_tokens - 1));
+    }
+    g.slots[i] = slot;
+  }
+  __syncthreads();
+#pragma unroll 4
+  for (int i = t; i < g.from.rows * width; i += kSoloThreads) {
+    const int r = i / width, k = i % width;
+    const bool ok = grows(r, have, want);
+    int32_t p = k < have ? page_at(g.from, r, k) : -1;
+    if (ok && k >= have && k < want) g.refs_out[p = list[before[r] + k - have]] = 1;
+    g.tables_out[i] = p;
+  }
+  for (int r = t; r < g.from.rows; r += kSoloThreads) g.lens_out[r] = lens[r] + (grows(r, have, want) ? counts[r] : 0);
+}
+
 // ---- compact -------------------------------------------------------------------------------------------------------------
 
 struct Compact {
@@ -402,8 +562,45 @@ __global__ __launch_bounds__(kThreads) void compact_refs(Compact c) {
     }
   }
 }
-template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, int32_t entry_wgs, int32_t parts) {
-  if ((int)blockIdx.x < entry_wgs) {
+// All of the books by one workgroup.
+__global__ __launch_bounds__(kSoloThreads) void compact_solo(Compact c) {
+  __shared__ int32_t refs[kSoloPages], shared[kSoloWaves], from[kSoloPages / 2], to[kSoloPages / 2];
+  const int t = threadIdx.x, pages = c.n_pages;
+  int32_t live = 0, all;
+  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
+    const int i = i0 + t;
+    if (i < pages) refs[i] = c.refs[i];
+    rank_of(i < pages && refs[i] != 0, shared, &all);
+    live += all;
+  }
+  int32_t movers = 0, room = 0;
+  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
+    const int i = i0 + t;
+    const bool is = i < pages && refs[i] != 0, moves = is && i >= live, takes = i < pages && !is && i < live;
+    // a page either moves or takes, and all that take come first
+    const int32_t at = rank_of(moves || takes, shared, &all);
+    if (takes) to[room + at] = i;
+    int32_t low;
+    rank_of(takes, shared, &low);
+    if (moves) from[movers + at - low] = i;
+    room += low, movers += all - low;
+    if (i < pages) {
+      c.places[i] = is && !moves ? i : -1;
+      if (!moves && !takes) c.refs_out[i] = refs[i];
+    }
+  }
+  __syncthreads();
+  for (int k = t; k < movers; k += kSoloThreads) {
+    const int32_t a = from[k], b = to[k];
+    c.from[k] = a, c.to[k] = b;
+    c.refs_out[b] = refs[a], c.refs_out[a] = 0;
+    c.places[a] = b;
+  }
+  if (t == 0) c.totals[0] = movers, *c.live = live;
+}
+// entry_wgs: workgroups that rewrite tables; the others copy
+template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, uint32_t entry_wgs, uint32_t parts) {
+  if (blockIdx.x < entry_wgs) {
     for (int k = 0; k < HF_MAX_TABLES; ++k)
       for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < c.n_entries[k]; i += (int64_t)entry_wgs * kThreads) {
         const int32_t p = c.entries[k][i];
@@ -411,11 +608,9 @@ template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_app
       }
     return;
   }
-  const int64_t items = c.totals[0] * buffers.n * parts;
-  for (int64_t i = (int64_t)blockIdx.x - entry_wgs; i < items; i += gridDim.x - entry_wgs) {
-    const int64_t part = i % parts, b = i / parts % buffers.n, k = i / parts / buffers.n;
-    copy_part<kVecBytes>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
-  }
+  each_part(c.totals[0], buffers.n, parts, blockIdx.x - entry_wgs, gridDim.x - entry_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
+    copy_part<kVecBytes, true>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
+  });
 }
 
 // ---- on the host ---------------------------------------------------------------------------------------------------------
@@ -445,8 +640,9 @@ Buffers buffers_of(const hf_page_pool &pool) {
   for (int i = 0; i < pool.n_caches; ++i) b.at[b.n++] = pool.caches[i].k, b.at[b.n++] = pool.caches[i].v;
   return b;
 }
-int32_t parts_of(const hf_kv_cache &c, int vec) { return (int32_t)up((int64_t)c.n_kv_heads * c.page_tokens * c.head_dim / vec, kThreads * kInFlight); }
-constexpr int64_t kMostCopyWgs = 4096, kMostRowWgs = 2048;
+uint32_t parts_of(const hf_kv_cache &c, int vec) { return (uint32_t)up((int64_t)c.n_kv_heads * c.page_tokens * c.head_dim / vec, kThreads * kInFlight); }
+constexpr int64_t kMostCopyWgs = 16384, kMostRowWgs = 2048;
+constexpr int64_t kSoloEntries = 16384; // of tables and slots, in all
 
 // arrays of a workspace, one after another, each 16-byte aligned
 struct Room {
@@ -471,7 +667,7 @@ Fork fork_of(const hf_page_pool &pool, const hf_page_fork &a, Room &room) {
   f.want_sums = room.take<int64_t>(f.row_tiles);
   f.free_list = room.take<int32_t>(a.rows_out);
   f.want = room.take<int32_t>(a.rows_out);
-  f.wanting = room.take<int32_t>(a.rows_out);
+  f.moves = room.take<Move>(a.rows_out);
   f.totals = room.take<int64_t>(2);
   return f;
 }
@@ -527,12 +723,18 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *
   Room room = {static_cast<char *>(a.workspace)};
   const Fork f = fork_of(pool, a, room);
   const auto wgs = [](int64_t n, int64_t each) { return dim3((uint32_t)std::max<int64_t>(1, std::min(up(n, each), kMostRowWgs))); };
-  if (const hipError_t e = enqueue_kernel(fork_begin, wgs(f.from.n_pages, kThreads), kThreads, st, f)) return e;
-  if (const hipError_t e = enqueue_kernel(fork_count, wgs((int64_t)a.rows + a.rows_out, kWaves), kThreads, st, f)) return e;
-  if (const hipError_t e = enqueue_kernel(fork_sums, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
-  if (const hipError_t e = enqueue_kernel(fork_lists, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
-  const int32_t parts = parts_of(pool.caches[0], vec), row_wgs = wgs(a.rows_out, kWaves).x;
+  const bool solo = f.from.n_pages <= kSoloPages && std::max(a.rows, a.rows_out) <= kSoloRows && (int64_t)std::max(a.rows, a.rows_out) * a.width <= kSoloEntries;
+  if (solo) {
+    if (const hipError_t e = enqueue_kernel(fork_solo, dim3(1), kSoloThreads, st, f)) return e;
+  } else {
+    if (const hipError_t e = enqueue_kernel(fork_begin, wgs(f.from.n_pages, kThreads), kThreads, st, f)) return e;
+    if (const hipError_t e = enqueue_kernel(fork_count, wgs((int64_t)a.rows + a.rows_out, kWaves), kThreads, st, f)) return e;
+    if (const hipError_t e = enqueue_kernel(fork_sums, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
+    if (const hipError_t e = enqueue_kernel(fork_lists, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
+  }
+  const uint32_t parts = parts_of(pool.caches[0], vec), row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
   const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
+  if (row_wgs + copies == 0) return hipSuccess;
   return by_access(vec, [&](auto bytes) {
     return enqueue_kernel(fork_apply<decltype(bytes)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape_of(pool.caches[0], vec), row_wgs, parts);
   });
@@ -542,22 +744,29 @@ int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   Room room = {static_cast<char *>(a.workspace)};
   const Grow g = grow_of(pool, a, room);
+  if (g.from.n_pages <= kSoloPages && a.rows <= kSoloRows && g.list <= kSoloFresh && (int64_t)a.rows * ((int64_t)a.width + a.most) <= kSoloEntries)
+    return enqueue_kernel(grow_solo, dim3(1), kSoloThreads, st, g);
   if (const hipError_t e = enqueue_kernel(grow_sums, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
   if (const hipError_t e = enqueue_kernel(grow_lists, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
-  return enqueue_kernel(grow_apply, dim3((uint32_t)std::min(up(a.rows, kWaves), kMostRowWgs)), kThreads, st, g);
+  return enqueue_kernel(grow_apply, dim3((uint32_t)std::max<int64_t>(1, std::min(up(a.rows, kWaves), kMostRowWgs))), kThreads, st, g);
 }
 
 int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, int vec, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   Room room = {static_cast<char *>(a.workspace)};
   const Compact c = compact_of(pool, a, room);
-  if (const hipError_t e = enqueue_kernel(compact_sums, dim3(c.page_tiles), kThreads, st, c)) return e;
-  if (const hipError_t e = enqueue_kernel(compact_lists, dim3(c.page_tiles), kThreads, st, c)) return e;
-  if (const hipError_t e = enqueue_kernel(compact_refs, dim3((uint32_t)std::min(up(c.n_pages, kThreads), kMostRowWgs)), kThreads, st, c)) return e;
+  if (c.n_pages <= kSoloPages) {
+    if (const hipError_t e = enqueue_kernel(compact_solo, dim3(1), kSoloThreads, st, c)) return e;
+  } else {
+    if (const hipError_t e = enqueue_kernel(compact_sums, dim3(c.page_tiles), kThreads, st, c)) return e;
+    if (const hipError_t e = enqueue_kernel(compact_lists, dim3(c.page_tiles), kThreads, st, c)) return e;
+    if (const hipError_t e = enqueue_kernel(compact_refs, dim3((uint32_t)std::min(up(c.n_pages, kThreads), kMostRowWgs)), kThreads, st, c)) return e;
+  }
   int64_t most = 0;
   for (const int64_t n : c.n_entries) most = std::max(most, n);
-  const int32_t parts = parts_of(pool.caches[0], vec), entry_wgs = (int32_t)std::min(up(most, kThreads), kMostRowWgs);
-  const int64_t copies = std::max<int64_t>(1, std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs));
+  const uint32_t parts = parts_of(pool.caches[0], vec), entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
+  const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
+  if (entry_wgs + copies == 0) return hipSuccess;
   return by_access(vec, [&](auto bytes) {
     return enqueue_kernel(compact_apply<decltype(bytes)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape_of(pool.caches[0], vec),
                           pool.caches[0].page_tokens, entry_wgs, parts);

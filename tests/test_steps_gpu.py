@@ -411,6 +411,11 @@ POOLS = [
     (128, 9, 1, 4, 2, "f16", "tokens", 0, 2, 2),
     (1, 5000, 1, 4, 4, "bf16", "heads", 0, 700, 9),
     (1, 300, 8, 256, 256, "bf16", "heads", 0, 20, 3),
+    # more rows, entries or pages than one workgroup keeps the books of
+    (2, 9000, 2, 4, 8, "f16", "heads", 0, 2500, 3),
+    (2, 3000, 2, 4, 8, "bf16", "tokens", 0, 50, 350),
+    (3, 17001, 1, 4, 4, "bf16", "heads", 0, 90, 150),
+    (1, 16384, 1, 8, 2, "bf16", "heads", 0, 1000, 16),
 ]
 
 
