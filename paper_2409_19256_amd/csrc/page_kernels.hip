@@ -113,8 +113,11 @@ template <int kVecBytes, bool kOnce> __device__ __forceinline__ void copy_part(v
 struct Move {
   int32_t from, tokens;
 };
-// Moves dealt out by parts of a page: f(move, buffer, part) for every `wgs`-th, from `wg` on
+// Moves dealt out by parts of a page: f(move, buffer, part) for every `wgs`-th, from `wg` on.  The parts of a page go to one XCD (workgroups go round them by eights):
+// 1024 pages of 512 KiB in four buffers, 245 of them moved, 187 us for 205.
 template <typename F> __device__ __forceinline__ void each_part(int64_t moves, uint32_t buffers, uint32_t parts, uint32_t wg, uint32_t wgs, const F &f) {
+  const uint32_t turn = 8 * parts;
+  if (wg < wgs / turn * turn) wg = wg / turn * turn + wg % 8 * parts + wg % turn / 8;
   const uint32_t per = buffers * parts, step = wgs / per, more = wgs % per;
   int64_t k = wg / per;
   for (uint32_t i = wg % per; k < moves; k += step, i += more) {
@@ -255,26 +258,54 @@ template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(
 
 // All of the books by one workgroup, counts in shared memory.
 constexpr int kSoloThreads = 1024, kSoloWaves = kSoloThreads / kWave, kSoloPages = 16384, kSoloRows = 2048;
-// how many of the lanes in front have `is`, and in all; `shared` holds one number a wavefront and may be used again at once
-__device__ __forceinline__ int32_t rank_of(bool is, int32_t *shared, int32_t *all) {
-  const uint64_t mask = __ballot(is);
-  const int wave = threadIdx.x / kWave;
-  if (threadIdx.x % kWave == 0) shared[wave] = __popcll(mask);
-  __syncthreads();
-  int32_t base = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < kSoloWaves; ++w) {
-    const int32_t n = shared[w];
-    base += w < wave ? n : 0;
-    total += n;
-  }
-  __syncthreads();
-  *all = total;
-  return base + __popcll(mask & ((1ull << threadIdx.x % kWave) - 1));
+constexpr int kSoloEach = kSoloPages / kSoloThreads; // pages of a lane, one after another
+// two numbers a lane, summed over the lanes in front and in all; for one use of `shared`
+struct Pair {
+  int32_t a, b;
+};
+template <int kControl, int kRows> __device__ __forceinline__ int32_t from_front(int32_t x) { return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xF, false); }
+// with the lanes in front: 1, 2, 4 and 8 further in each row of 16, then the rows' ends
+__device__ __forceinline__ int32_t row_sums(int32_t x) {
+  x += from_front<0x111, 0xF>(x);
+  x += from_front<0x112, 0xF>(x);
+  x += from_front<0x114, 0xF>(x);
+  return x + from_front<0x118, 0xF>(x);
 }
+__device__ __forceinline__ int32_t wave_sums(int32_t x) {
+  x = row_sums(x);
+  x += from_front<0x142, 0xA>(x);
+  return x + from_front<0x143, 0xC>(x);
+}
+__device__ __forceinline__ Pair sums_before(Pair x, Pair *shared, Pair *all) {
+  static_assert(kSoloWaves <= 16, "the wavefronts' sums lie in one row of lanes");
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Pair upto = {wave_sums(x.a), wave_sums(x.b)};
+  if (lane == kWave - 1) shared[wave] = upto;
+  __syncthreads();
+  const Pair theirs = lane < kSoloWaves ? shared[lane] : Pair{0, 0}, sums = {row_sums(theirs.a), row_sums(theirs.b)};
+  *all = {__builtin_amdgcn_readlane(sums.a, kSoloWaves - 1), __builtin_amdgcn_readlane(sums.b, kSoloWaves - 1)};
+  const Pair base = {wave ? __builtin_amdgcn_readlane(sums.a, wave - 1) : 0, wave ? __builtin_amdgcn_readlane(sums.b, wave - 1) : 0};
+  return {base.a + upto.a - x.a, base.b + upto.b - x.b};
+}
+// a lane's pages of an array, four at a time: loaded as far as they go, the others are `none`
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_any __attribute__((aligned(4)));
+__device__ __forceinline__ i32x4 four_of(const int32_t *from, int i, int n, int32_t none) {
+  if (i + 4 <= n) return *reinterpret_cast<const i32x4_any *>(from + i);
+  i32x4 v = none;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) v[e] = from[i + e];
+  return v;
+}
+__device__ __forceinline__ int each_of(int pages) { return (pages + 4 * kSoloThreads - 1) / (4 * kSoloThreads) * 4; } // of a lane, a multiple of four
+
 __global__ __launch_bounds__(kSoloThreads) void fork_solo(Fork f) {
-  __shared__ int32_t refs[kSoloPages], first[kSoloPages], lens[kSoloRows], parents[kSoloRows], shared[kSoloWaves];
+  __shared__ __attribute__((aligned(16))) int32_t refs[kSoloPages], first[kSoloPages];
+  __shared__ int32_t lens[kSoloRows], parents[kSoloRows];
+  __shared__ Pair shared[kSoloWaves];
   const int t = threadIdx.x, width = f.from.width, pages = f.from.n_pages, part = (1 << f.from.shift) - 1;
+#pragma unroll 4
   for (int i = t; i < pages; i += kSoloThreads) refs[i] = f.refs[i], first[i] = INT32_MAX;
   for (int r = t; r < f.from.rows; r += kSoloThreads) lens[r] = (int32_t)len_of(f.from, r);
   for (int r = t; r < f.rows_out; r += kSoloThreads) parents[r] = (int32_t)parent_of(f, r);
@@ -296,24 +327,49 @@ __global__ __launch_bounds__(kSoloThreads) void fork_solo(Fork f) {
         else atomicMin(&first[p], r);
       }
   }
+  // a lane's rows and pages lie one after another: what stands in front of them is one sum
+  constexpr int kRows = kSoloRows / kSoloThreads;
+  const int rows_each = (f.rows_out + kSoloThreads - 1) / kSoloThreads;
+  int32_t open[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int r = t * rows_each + k;
+    open[k] = k < rows_each && r < f.rows_out ? open_at(parents[r]) : -1;
+  }
   __syncthreads();
-  int32_t wanted = 0, free = 0, all;
-  for (int r0 = 0; r0 < f.rows_out; r0 += kSoloThreads) {
-    const int r = r0 + t, p = r < f.rows_out ? open_at(parents[r]) : -1;
-    const bool wants = p >= 0 && first[p] != r;
-    const int32_t at = wanted + rank_of(wants, shared, &all);
-    if (r < f.rows_out) f.want[r] = wants ? at : -1;
-    if (wants) f.moves[at] = {p, len_at(parents[r]) & part};
-    wanted += all;
+  Pair mine = {0, 0}, all;
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    if (open[k] >= 0 && first[open[k]] == t * rows_each + k) open[k] = -1;
+    mine.a += open[k] >= 0;
   }
-  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
-    const int i = i0 + t;
-    const bool kept = i < pages && first[i] != INT32_MAX, is = i < pages && refs[i] == 0 && !kept;
-    const int32_t at = free + rank_of(is, shared, &all);
-    if (is && at < wanted) f.free_list[at] = i;
-    if (kept) ++refs[i];
-    free += all;
+  const int each = each_of(pages);
+  uint32_t is_free = 0;
+#pragma unroll
+  for (int k = 0; k < kSoloEach; k += 4) {
+    const int i = t * each + k;
+    if (k >= each || i >= pages) break;
+    const i32x4 n = *reinterpret_cast<const i32x4 *>(refs + i), held = *reinterpret_cast<const i32x4 *>(first + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (i + e >= pages) continue;
+      if (held[e] != INT32_MAX) refs[i + e] = n[e] + 1; // the first row that goes on in it has it
+      else if (n[e] == 0) is_free |= 1u << (k + e);
+    }
   }
+  mine.b = __popc(is_free);
+  Pair at = sums_before(mine, shared, &all);
+  const int32_t wanted = all.a, free = all.b;
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int r = t * rows_each + k;
+    if (k >= rows_each || r >= f.rows_out) continue;
+    f.want[r] = open[k] >= 0 ? at.a : -1;
+    if (open[k] >= 0) f.moves[at.a++] = {open[k], len_at(parents[r]) & part};
+  }
+  for (uint32_t left = is_free; left; left &= left - 1, ++at.b)
+    if (at.b < wanted) f.free_list[at.b] = t * each + __builtin_ctz(left);
+  if (t == 0) f.totals[0] = free, f.totals[1] = wanted;
   __syncthreads();
 #pragma unroll 4
   for (int i = t; i < f.rows_out * width; i += kSoloThreads) {
@@ -325,7 +381,6 @@ __global__ __launch_bounds__(kSoloThreads) void fork_solo(Fork f) {
   for (int r = t; r < f.rows_out; r += kSoloThreads) f.lens_out[r] = f.want[r] >= free ? 0 : len_at(parents[r]);
   __syncthreads();
   for (int i = t; i < pages; i += kSoloThreads) f.refs_out[i] = refs[i];
-  if (t == 0) f.totals[0] = free, f.totals[1] = wanted;
 }
 
 // ---- grow ----------------------------------------------------------------------------------------------------------------
@@ -436,43 +491,46 @@ __global__ __launch_bounds__(kThreads) void grow_apply(Grow g) {
 // All of it by one workgroup.
 constexpr int kSoloFresh = 8192; // fresh pages that it can hand out
 __global__ __launch_bounds__(kSoloThreads) void grow_solo(Grow g) {
-  __shared__ int32_t list[kSoloFresh], before[kSoloRows], lens[kSoloRows], counts[kSoloRows], shared[kSoloWaves];
+  __shared__ int32_t list[kSoloFresh], before[kSoloRows], lens[kSoloRows], counts[kSoloRows];
+  __shared__ Pair shared[kSoloWaves];
   const int t = threadIdx.x, width = g.from.width, pages = g.from.n_pages, shift = g.from.shift, page_tokens = 1 << shift;
-  int32_t wanted = 0, free = 0, all;
-  for (int r0 = 0; r0 < g.from.rows; r0 += kSoloThreads) {
-    const int r = r0 + t;
-    int32_t need = 0;
-    if (r < g.from.rows) {
-      const Growth x = growth_of(g, r);
-      need = (int32_t)x.need();
-      lens[r] = (int32_t)x.len, counts[r] = x.fits ? x.count : -1;
-    }
-    int32_t upto = need; // sums over the wavefront, then over the workgroup
-    for (int d = 1; d < kWave; d *= 2) {
-      const int32_t y = __shfl_up(upto, d);
-      if (t % kWave >= d) upto += y;
-    }
-    if (t % kWave == kWave - 1) shared[t / kWave] = upto;
-    __syncthreads();
-    int32_t base = 0;
-    all = 0;
+  // a lane's rows and pages lie one after another: what stands in front of them is one sum
+  const int each = each_of(pages), rows_each = (g.from.rows + kSoloThreads - 1) / kSoloThreads;
+  i32x4 refs[kSoloEach / 4];
 #pragma unroll
-    for (int w = 0; w < kSoloWaves; ++w) {
-      base += w < t / kWave ? shared[w] : 0;
-      all += shared[w];
-    }
-    __syncthreads();
-    if (r < g.from.rows) before[r] = wanted + base + upto - need;
-    wanted += all;
+  for (int k = 0; k < kSoloEach; k += 4)
+    if (k < each) refs[k / 4] = four_of(g.refs, t * each + k, pages, 1);
+  constexpr int kRows = kSoloRows / kSoloThreads;
+  int32_t need[kRows];
+  Pair mine = {0, 0}, all;
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int r = t * rows_each + k;
+    need[k] = 0;
+    if (k >= rows_each || r >= g.from.rows) continue;
+    const Growth x = growth_of(g, r);
+    need[k] = (int32_t)x.need();
+    lens[r] = (int32_t)x.len, counts[r] = x.fits ? x.count : -1;
+    mine.a += need[k];
   }
-  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
-    const int i = i0 + t;
-    const int32_t refs = i < pages ? g.refs[i] : 1;
-    const int32_t at = free + rank_of(refs == 0, shared, &all);
-    const bool taken = refs == 0 && at < wanted;
-    if (taken) list[at] = i;
-    if (i < pages && g.refs_out != g.refs) g.refs_out[i] = refs;
-    free += all;
+  uint32_t is_free = 0;
+#pragma unroll
+  for (int k = 0; k < kSoloEach; ++k)
+    if (k < each && refs[k / 4][k % 4] == 0) is_free |= 1u << k;
+  mine.b = __popc(is_free);
+  Pair at = sums_before(mine, shared, &all);
+  const int32_t wanted = all.a, free = all.b;
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int r = t * rows_each + k;
+    if (k < rows_each && r < g.from.rows) before[r] = at.a, at.a += need[k];
+  }
+  for (uint32_t left = is_free; left; left &= left - 1, ++at.b)
+    if (at.b < wanted) list[at.b] = t * each + __builtin_ctz(left);
+  if (g.refs_out != g.refs) {
+#pragma unroll
+    for (int k = 0; k < kSoloEach; ++k)
+      if (const int i = t * each + k; k < each && i < pages) g.refs_out[i] = refs[k / 4][k % 4];
   }
   __syncthreads();
   const auto grows = [&](int r, int32_t &have, int32_t &want) {
@@ -564,39 +622,48 @@ __global__ __launch_bounds__(kThreads) void compact_refs(Compact c) {
 }
 // All of the books by one workgroup.
 __global__ __launch_bounds__(kSoloThreads) void compact_solo(Compact c) {
-  __shared__ int32_t refs[kSoloPages], shared[kSoloWaves], from[kSoloPages / 2], to[kSoloPages / 2];
-  const int t = threadIdx.x, pages = c.n_pages;
-  int32_t live = 0, all;
-  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
-    const int i = i0 + t;
-    if (i < pages) refs[i] = c.refs[i];
-    rank_of(i < pages && refs[i] != 0, shared, &all);
-    live += all;
+  __shared__ int32_t from[kSoloPages / 2], to[kSoloPages / 2], refs_of[kSoloPages / 2], staying;
+  __shared__ Pair shared[kSoloWaves];
+  const int t = threadIdx.x, pages = c.n_pages, each = each_of(pages); // a lane's pages lie one after another
+  i32x4 refs[kSoloEach / 4];
+  Pair mine = {0, 0}, all;
+#pragma unroll
+  for (int k = 0; k < kSoloEach; k += 4)
+    if (k < each) refs[k / 4] = four_of(c.refs, t * each + k, pages, 0);
+#pragma unroll
+  for (int k = 0; k < kSoloEach; ++k)
+    if (k < each) mine.a += refs[k / 4][k % 4] != 0;
+  int32_t before = sums_before(mine, shared, &all).a; // in use in front of a page
+  const int32_t live = all.a;
+  if (live >= t * each && live < (t + 1) * each) { // those in use below number `live`, which stay
+    int32_t n = before;
+#pragma unroll
+    for (int k = 0; k < kSoloEach; ++k)
+      if (k < each && t * each + k < live) n += refs[k / 4][k % 4] != 0;
+    staying = n;
   }
-  int32_t movers = 0, room = 0;
-  for (int i0 = 0; i0 < pages; i0 += kSoloThreads) {
-    const int i = i0 + t;
-    const bool is = i < pages && refs[i] != 0, moves = is && i >= live, takes = i < pages && !is && i < live;
-    // a page either moves or takes, and all that take come first
-    const int32_t at = rank_of(moves || takes, shared, &all);
-    if (takes) to[room + at] = i;
-    int32_t low;
-    rank_of(takes, shared, &low);
-    if (moves) from[movers + at - low] = i;
-    room += low, movers += all - low;
-    if (i < pages) {
-      c.places[i] = is && !moves ? i : -1;
-      if (!moves && !takes) c.refs_out[i] = refs[i];
-    }
+  if (t == 0 && live >= kSoloThreads * each) staying = live;
+  __syncthreads();
+  const int32_t stay = staying;
+#pragma unroll
+  for (int k = 0; k < kSoloEach; ++k) {
+    const int i = t * each + k;
+    if (k >= each || i >= pages) continue;
+    const int32_t n = refs[k / 4][k % 4];
+    if (n && i >= live) from[before - stay] = i, refs_of[before - stay] = n;
+    else if (!n && i < live) to[i - before] = i;
+    else c.refs_out[i] = n;
+    if (!(n && i >= live)) c.places[i] = n ? i : -1;
+    before += n != 0;
   }
   __syncthreads();
-  for (int k = t; k < movers; k += kSoloThreads) {
+  for (int k = t; k < live - stay; k += kSoloThreads) {
     const int32_t a = from[k], b = to[k];
     c.from[k] = a, c.to[k] = b;
-    c.refs_out[b] = refs[a], c.refs_out[a] = 0;
+    c.refs_out[b] = refs_of[k], c.refs_out[a] = 0;
     c.places[a] = b;
   }
-  if (t == 0) c.totals[0] = movers, *c.live = live;
+  if (t == 0) c.totals[0] = live - stay, *c.live = live;
 }
 // entry_wgs: workgroups that rewrite tables; the others copy
 template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, uint32_t entry_wgs, uint32_t parts) {
