@@ -50,6 +50,45 @@ __device__ __forceinline__ int64_t sum_of(const int64_t *sums, int64_t n, int64_
   return sum_block(x, shared);
 }
 
+// two numbers a lane, summed over the lanes in front and in all; for one use of `shared`
+struct Pair {
+  int32_t a, b;
+};
+template <int kControl, int kRows> __device__ __forceinline__ int32_t from_front(int32_t x) { return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xF, false); }
+// with the lanes in front: 1, 2, 4 and 8 further in each row of 16, then the rows' ends
+__device__ __forceinline__ int32_t row_sums(int32_t x) {
+  x += from_front<0x111, 0xF>(x);
+  x += from_front<0x112, 0xF>(x);
+  x += from_front<0x114, 0xF>(x);
+  return x + from_front<0x118, 0xF>(x);
+}
+__device__ __forceinline__ int32_t wave_sums(int32_t x) {
+  x = row_sums(x);
+  x += from_front<0x142, 0xA>(x);
+  return x + from_front<0x143, 0xC>(x);
+}
+template <int kWaves> __device__ __forceinline__ Pair sums_before(Pair x, Pair (&shared)[kWaves], Pair *all) {
+  static_assert(kWaves <= 16, "the wavefronts' sums lie in one row of lanes");
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Pair upto = {wave_sums(x.a), wave_sums(x.b)};
+  if (lane == kWave - 1) shared[wave] = upto;
+  __syncthreads();
+  const Pair theirs = lane < kWaves ? shared[lane] : Pair{0, 0}, sums = {row_sums(theirs.a), row_sums(theirs.b)};
+  *all = {__builtin_amdgcn_readlane(sums.a, kWaves - 1), __builtin_amdgcn_readlane(sums.b, kWaves - 1)};
+  const Pair base = {wave ? __builtin_amdgcn_readlane(sums.a, wave - 1) : 0, wave ? __builtin_amdgcn_readlane(sums.b, wave - 1) : 0};
+  return {base.a + upto.a - x.a, base.b + upto.b - x.b};
+}
+// a lane's pages of an array, four at a time: loaded as far as they go, the others are `none`
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_any __attribute__((aligned(4)));
+__device__ __forceinline__ i32x4 four_of(const int32_t *from, int64_t i, int64_t n, int32_t none) {
+  if (i + 4 <= n) return *reinterpret_cast<const i32x4_any *>(from + i);
+  i32x4 v = none;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (i + e < n) v[e] = from[i + e];
+  return v;
+}
 // Tables of page numbers, and what of a row counts.
 struct Tables {
   const int32_t *entries, *lens;
@@ -198,17 +237,25 @@ __global__ __launch_bounds__(kThreads) void fork_sums(Fork f) {
 }
 __global__ __launch_bounds__(kThreads) void fork_lists(Fork f) {
   __shared__ int64_t shared[kWaves];
+  __shared__ Pair pairs[kWaves];
   int64_t all;
   if ((int)blockIdx.x < f.page_tiles) {
-    int64_t base = sum_of(f.free_sums, blockIdx.x, shared);
+    int32_t base = (int32_t)sum_of(f.free_sums, blockIdx.x, shared);
     const int64_t begin = blockIdx.x * f.page_tile, end = min(begin + f.page_tile, (int64_t)f.from.n_pages);
-    for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
-      const int64_t i = i0 + threadIdx.x;
-      const bool is = i < end && is_free(f, i);
-      const int64_t at = base + sum_before(is, shared, &all);
-      if (is && at < f.rows_out) f.free_list[at] = (int32_t)i;
-      if (i < end && f.first[i] != INT32_MAX) ++f.refs_out[i];
-      base += all;
+    for (int64_t i0 = begin; i0 < end; i0 += 4 * kThreads) {
+      const int64_t i = i0 + 4 * threadIdx.x;
+      const i32x4 refs = four_of(f.refs_out, i, end, 1), first = four_of(f.first, i, end, INT32_MAX);
+      Pair mine = {0, 0}, sums;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine.a += refs[e] == 0 && first[e] == INT32_MAX;
+      int32_t at = base + sums_before(mine, pairs, &sums).a;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (first[e] != INT32_MAX) f.refs_out[i + e] = refs[e] + 1;
+        else if (refs[e] == 0 && at++ < f.rows_out) f.free_list[at - 1] = (int32_t)(i + e);
+      }
+      base += sums.a;
+      __syncthreads();
     }
     if ((int)blockIdx.x == f.page_tiles - 1 && threadIdx.x == 0) f.totals[0] = base;
   } else {
@@ -257,47 +304,8 @@ template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(
 }
 
 // All of the books by one workgroup, counts in shared memory.
-constexpr int kSoloThreads = 1024, kSoloWaves = kSoloThreads / kWave, kSoloPages = 16384, kSoloRows = 2048;
+constexpr int kSoloThreads = 1024, kSoloWaves = kSoloThreads / kWave, kSoloPages = 8192, kSoloRows = 2048;
 constexpr int kSoloEach = kSoloPages / kSoloThreads; // pages of a lane, one after another
-// two numbers a lane, summed over the lanes in front and in all; for one use of `shared`
-struct Pair {
-  int32_t a, b;
-};
-template <int kControl, int kRows> __device__ __forceinline__ int32_t from_front(int32_t x) { return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xF, false); }
-// with the lanes in front: 1, 2, 4 and 8 further in each row of 16, then the rows' ends
-__device__ __forceinline__ int32_t row_sums(int32_t x) {
-  x += from_front<0x111, 0xF>(x);
-  x += from_front<0x112, 0xF>(x);
-  x += from_front<0x114, 0xF>(x);
-  return x + from_front<0x118, 0xF>(x);
-}
-__device__ __forceinline__ int32_t wave_sums(int32_t x) {
-  x = row_sums(x);
-  x += from_front<0x142, 0xA>(x);
-  return x + from_front<0x143, 0xC>(x);
-}
-__device__ __forceinline__ Pair sums_before(Pair x, Pair *shared, Pair *all) {
-  static_assert(kSoloWaves <= 16, "the wavefronts' sums lie in one row of lanes");
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const Pair upto = {wave_sums(x.a), wave_sums(x.b)};
-  if (lane == kWave - 1) shared[wave] = upto;
-  __syncthreads();
-  const Pair theirs = lane < kSoloWaves ? shared[lane] : Pair{0, 0}, sums = {row_sums(theirs.a), row_sums(theirs.b)};
-  *all = {__builtin_amdgcn_readlane(sums.a, kSoloWaves - 1), __builtin_amdgcn_readlane(sums.b, kSoloWaves - 1)};
-  const Pair base = {wave ? __builtin_amdgcn_readlane(sums.a, wave - 1) : 0, wave ? __builtin_amdgcn_readlane(sums.b, wave - 1) : 0};
-  return {base.a + upto.a - x.a, base.b + upto.b - x.b};
-}
-// a lane's pages of an array, four at a time: loaded as far as they go, the others are `none`
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef i32x4 i32x4_any __attribute__((aligned(4)));
-__device__ __forceinline__ i32x4 four_of(const int32_t *from, int i, int n, int32_t none) {
-  if (i + 4 <= n) return *reinterpret_cast<const i32x4_any *>(from + i);
-  i32x4 v = none;
-#pragma unroll
-  for (int e = 0; e < 3; ++e)
-    if (i + e < n) v[e] = from[i + e];
-  return v;
-}
 __device__ __forceinline__ int each_of(int pages) { return (pages + 4 * kSoloThreads - 1) / (4 * kSoloThreads) * 4; } // of a lane, a multiple of four
 
 __global__ __launch_bounds__(kSoloThreads) void fork_solo(Fork f) {
@@ -435,16 +443,24 @@ __global__ __launch_bounds__(kThreads) void grow_sums(Grow g) {
 }
 __global__ __launch_bounds__(kThreads) void grow_lists(Grow g) {
   __shared__ int64_t shared[kWaves];
+  __shared__ Pair pairs[kWaves];
   int64_t all;
   if ((int)blockIdx.x < g.page_tiles) {
-    int64_t base = sum_of(g.free_sums, blockIdx.x, shared);
     const int64_t begin = blockIdx.x * g.page_tile, end = min(begin + g.page_tile, (int64_t)g.from.n_pages);
-    for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
-      const int64_t i = i0 + threadIdx.x;
-      const bool is = i < end && g.refs_out[i] == 0;
-      const int64_t at = base + sum_before(is, shared, &all);
-      if (is && at < g.list) g.free_list[at] = (int32_t)i;
-      base += all;
+    i32x4 refs = four_of(g.refs_out, begin + 4 * threadIdx.x, end, 1);
+    int32_t base = (int32_t)sum_of(g.free_sums, blockIdx.x, shared);
+    for (int64_t i0 = begin; i0 < end; i0 += 4 * kThreads) {
+      const int64_t i = i0 + 4 * threadIdx.x;
+      if (i0 > begin) refs = four_of(g.refs_out, i, end, 1);
+      Pair mine = {0, 0}, sums;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine.a += refs[e] == 0;
+      int32_t at = base + sums_before(mine, pairs, &sums).a;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (refs[e] == 0 && at++ < g.list) g.free_list[at - 1] = (int32_t)(i + e);
+      base += sums.a;
+      __syncthreads();
     }
     if ((int)blockIdx.x == g.page_tiles - 1 && threadIdx.x == 0) g.totals[0] = base;
   } else {
@@ -482,7 +498,7 @@ __global__ __launch_bounds__(kThreads) void grow_apply(Grow g) {
         const int64_t p = k < x.have ? open : g.free_list[before + k - x.have];
         if (p >= 0) slot = (p << g.from.shift) + (at & (page_tokens - 1));
       }
-      g.slots[r * g.most + i] = slot;
+      __builtin_nontemporal_store(slot, g.slots + r * g.most + i); // (plain stores: 4096 rows of 1024 in 17.9 us for 15.7)
     }
     if (lane == 0) g.lens_out[r] = (int32_t)(ok ? x.len + x.count : x.len);
   }
@@ -586,24 +602,33 @@ __global__ __launch_bounds__(kThreads) void compact_sums(Compact c) {
 }
 __global__ __launch_bounds__(kThreads) void compact_lists(Compact c) {
   __shared__ int64_t shared[kWaves];
+  __shared__ Pair pairs[kWaves];
   const int64_t live = sum_of(c.live_sums, c.page_tiles, shared);
   // those in use below number `live`, which stay
   const int64_t whole = live / c.page_tile;
-  int64_t stay = 0, all;
+  int64_t stay = 0;
   for (int64_t i = whole * c.page_tile + threadIdx.x; i < live; i += kThreads) stay += c.refs[i] != 0;
   stay = sum_block(stay, shared) + sum_of(c.live_sums, whole, shared);
-  int64_t base = sum_of(c.live_sums, blockIdx.x, shared);
+  int32_t base = (int32_t)sum_of(c.live_sums, blockIdx.x, shared);
   const int64_t begin = blockIdx.x * c.page_tile, end = min(begin + c.page_tile, (int64_t)c.n_pages);
-  for (int64_t i0 = begin; i0 < end; i0 += kThreads) {
-    const int64_t i = i0 + threadIdx.x;
-    const bool is = i < end && c.refs[i] != 0;
-    const int64_t before = base + sum_before(is, shared, &all); // in use in front of page i
-    if (i < end) {
-      if (is && i >= live) c.from[before - stay] = (int32_t)i;
-      if (!is && i < live) c.to[i - before] = (int32_t)i;
-      c.places[i] = is && i < live ? (int32_t)i : -1;
+  for (int64_t i0 = begin; i0 < end; i0 += 4 * kThreads) {
+    const int64_t i = i0 + 4 * threadIdx.x;
+    const i32x4 refs = four_of(c.refs, i, end, 0);
+    Pair mine = {0, 0}, sums;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine.a += refs[e] != 0;
+    int32_t before = base + sums_before(mine, pairs, &sums).a; // in use in front of a page
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (i + e >= end) continue;
+      const bool is = refs[e] != 0;
+      if (is && i + e >= live) c.from[before - stay] = (int32_t)(i + e);
+      if (!is && i + e < live) c.to[i + e - before] = (int32_t)(i + e);
+      c.places[i + e] = is && i + e < live ? (int32_t)(i + e) : -1;
+      before += is;
     }
-    base += all;
+    base += sums.a;
+    __syncthreads();
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) c.totals[0] = live - stay, *c.live = (int32_t)live;
 }
@@ -709,7 +734,10 @@ Buffers buffers_of(const hf_page_pool &pool) {
 }
 uint32_t parts_of(const hf_kv_cache &c, int vec) { return (uint32_t)up((int64_t)c.n_kv_heads * c.page_tokens * c.head_dim / vec, kThreads * kInFlight); }
 constexpr int64_t kMostCopyWgs = 16384, kMostRowWgs = 2048;
-constexpr int64_t kSoloEntries = 16384; // of tables and slots, in all
+// One workgroup keeps the books of up to kSoloPages pages and kSoloEntries entries of tables (of tables and slots, twice as many): us, by one / by launches after one another, fork of 256 rows of 8, 31
+// and 60 pages 8.8 / 16.1, 16.0 / 17.3, 25.5 / 17.8; grow by one token of 256 rows in 4096 and 16384 pages 8.0 / 10.2, 15.1 / 10.8, by 900 of 16 rows 10.5 / 12.6; compact of 1024, 8192 and 16384 pages
+// 7.5 / 13.7, 16.3 / 18.7, 26.9 / 23.8.
+constexpr int64_t kSoloEntries = 8192;
 
 // arrays of a workspace, one after another, each 16-byte aligned
 struct Room {
@@ -811,7 +839,7 @@ int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   Room room = {static_cast<char *>(a.workspace)};
   const Grow g = grow_of(pool, a, room);
-  if (g.from.n_pages <= kSoloPages && a.rows <= kSoloRows && g.list <= kSoloFresh && (int64_t)a.rows * ((int64_t)a.width + a.most) <= kSoloEntries)
+  if (g.from.n_pages <= kSoloPages && a.rows <= kSoloRows && g.list <= kSoloFresh && (int64_t)a.rows * ((int64_t)a.width + a.most) <= 2 * kSoloEntries)
     return enqueue_kernel(grow_solo, dim3(1), kSoloThreads, st, g);
   if (const hipError_t e = enqueue_kernel(grow_sums, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
   if (const hipError_t e = enqueue_kernel(grow_lists, dim3(g.page_tiles + g.row_tiles), kThreads, st, g)) return e;
