@@ -233,7 +233,7 @@ template <typename T, int kThreads, int kPlaces, bool kOnce> __global__ __launch
   const double inv_t = in.inv_temperature, w = a.reverse;
   const bool others = !(st.s <= 0), rest = others && a.flags & HF_DISTILL_REST;
   // ln of the others' sum, relative to their own largest and to the row's
-  const double log_own = others ? (__builtin_amdgcn_logf(st.s) + (double)st.k - ((double)st.m - st.r) * c) * kLn2 : -INFINITY; // (the sum has 32 bits)
+  const double log_own = others ? log((double)st.s) + ((double)st.k - ((double)st.m - st.r) * c) * kLn2 : -INFINITY;
   const double log_others = others ? log_own + ((double)st.m - top) * inv_t : -INFINITY;
   const auto y_of = [&](int k) { return x_named[k] == -INFINITY ? -(double)INFINITY : ((double)x_named[k] - top) * inv_t; };
   double z = 0, q_sum = 0;

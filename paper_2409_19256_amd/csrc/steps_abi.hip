@@ -68,56 +68,54 @@ int check_pool(const hf_page_pool *p) {
   return HF_OK;
 }
 
-// Keys and values of a pool's caches, as places in memory.
-struct Buffers {
-  Place at[2 * HF_MAX_CACHES];
-  int n = 0;
+// Keys and values of a pool's caches, as places in memory: all alike but for where they begin.
+class Buffers {
+  Place one_;
+  uintptr_t begins_[2 * HF_MAX_CACHES]; // ascending
+  int n_ = 0;
+  bool apart_ = true; // one ends before the next begins
+  Place at(uintptr_t begin) const {
+    Place p = one_;
+    p.end += begin - p.begin, p.begin = begin;
+    return p;
+  }
+  void sort() {
+    if (!std::is_sorted(begins_, begins_ + n_)) std::sort(begins_, begins_ + n_);
+  }
+
+public:
   explicit Buffers(const hf_page_pool &pool) {
-    for (int i = 0; i < pool.n_caches; ++i) {
-      const hf_kv_cache &c = pool.caches[i];
-      const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
-      for (const void *p : {c.k, c.v}) {
-        if (n == 0) {
-          at[n] = place(p, dims, c.head_dim, 2);
-        } else {
-          at[n] = at[0];
-          at[n].end += reinterpret_cast<uintptr_t>(p) - at[n].begin, at[n].begin = reinterpret_cast<uintptr_t>(p);
-        }
-        ++n;
-      }
-    }
+    const hf_kv_cache &c = pool.caches[0];
+    const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
+    one_ = place(c.k, dims, c.head_dim, 2);
+    for (int i = 0; i < pool.n_caches; ++i)
+      for (const void *p : {pool.caches[i].k, pool.caches[i].v}) begins_[n_++] = reinterpret_cast<uintptr_t>(p);
+    sort();
+    for (int i = 1; i < n_; ++i) apart_ = apart_ && begins_[i] - begins_[i - 1] >= one_.end - one_.begin;
   }
   bool meet(const Place &p) const {
-    return std::any_of(at, at + n, [&](const Place &q) { return overlap(p, q); });
+    const uintptr_t *end = std::lower_bound(begins_, begins_ + n_, p.end), *b = begins_; // those that begin before it ends
+    if (apart_) b = std::lower_bound(b, end, p.begin - std::min(p.begin, one_.end - one_.begin));
+    return std::any_of(b, end, [&](uintptr_t q) { return overlap(p, at(q)); });
   }
   // Whether two of them share a byte.  Mostly they lie one after another; where they lie between one another's pages, only those whose beginnings are
   // nearer than a page's own span, page strides left out, have to be looked at.
-  bool meet_one_another() const {
+  bool meet_one_another() {
+    if (apart_) return false;
+    const Dim &pages = one_.dims[0], &heads = one_.dims[1], &tokens = one_.dims[2];
+    const int64_t reach = (heads.n - 1) * heads.stride + (tokens.n - 1) * tokens.stride + one_.inner;
+    const uintptr_t period = pages.n > 1 && pages.stride >= reach ? pages.stride : 0;
     struct Begin {
-      uintptr_t at;
-      int i;
+      uintptr_t in_period, at;
     } begins[2 * HF_MAX_CACHES];
-    const auto sort = [&] {
-      const auto less = [](const Begin &a, const Begin &b) { return a.at < b.at; };
-      if (!std::is_sorted(begins, begins + n, less)) std::sort(begins, begins + n, less);
-    };
-    for (int i = 0; i < n; ++i) begins[i] = {at[i].begin, i};
-    sort();
-    bool apart = true;
-    for (int i = 1; i < n; ++i) apart = apart && at[begins[i - 1].i].end <= at[begins[i].i].begin;
-    if (apart) return false;
-    const Dim &pages = at[0].dims[0], &heads = at[0].dims[1], &tokens = at[0].dims[2];
-    const int64_t reach = (heads.n - 1) * heads.stride + (tokens.n - 1) * tokens.stride + at[0].inner;
-    const int64_t period = pages.n > 1 && pages.stride >= reach ? pages.stride : 0;
-    if (period)
-      for (int i = 0; i < n; ++i) begins[i] = {at[i].begin % period, i};
-    sort();
-    for (int i = 0; i < n; ++i)
-      for (int k = 1; k < n; ++k) {
-        const int j = (i + k) % n;
+    for (int i = 0; i < n_; ++i) begins[i] = {period ? begins_[i] % period : begins_[i], begins_[i]};
+    std::sort(begins, begins + n_, [](const Begin &x, const Begin &y) { return x.in_period < y.in_period; });
+    for (int i = 0; i < n_; ++i)
+      for (int k = 1; k < n_; ++k) {
+        const int j = (i + k) % n_;
         if (!period && j < i) break;
-        if (period && (begins[j].at + (j < i ? period : 0)) - begins[i].at >= (uint64_t)reach) break;
-        if (overlap(at[begins[i].i], at[begins[j].i])) return true;
+        if (period && begins[j].in_period + (j < i ? period : 0) - begins[i].in_period >= (uint64_t)reach) break;
+        if (overlap(at(begins[i].at), at(begins[j].at))) return true;
       }
     return false;
   }
@@ -252,7 +250,7 @@ int hf_fork_pages(const hf_page_pool *pool, const hf_page_fork *args, void *hip_
                             {"the workspace overlaps an input or an output", array(a.workspace, (int64_t)need, 1)},
                             {"refs_out overlaps an input or another output and is not refs", array(a.refs_out, pages, 4)}};
   if (const char *what = first_overlap(outputs, {tables, lens, parents, a.refs == a.refs_out ? Place{} : refs})) return set_error(HF_EINVAL, what);
-  const Buffers buffers(*pool);
+  Buffers buffers(*pool);
   for (const Place &p : {tables, lens, parents, refs})
     if (buffers.meet(p)) return set_error(HF_EINVAL, "a cache overlaps an input");
   for (const Output &o : outputs)
@@ -323,7 +321,7 @@ int hf_compact_pages(const hf_page_pool *pool, const hf_page_compact *args, void
   for (int i = 0; i < HF_MAX_TABLES; ++i)
     for (size_t j = 0; j < sizeof(outputs) / sizeof(outputs[0]); ++j)
       if (!((int)j == i && a.entries[i] == a.entries_out[i]) && overlap(in[i], outputs[j].place)) return set_error(HF_EINVAL, "entries overlap an output that is not their own");
-  const Buffers buffers(*pool);
+  Buffers buffers(*pool);
   for (const Place &p : {refs, in[0], in[1], in[2], in[3]})
     if (buffers.meet(p)) return set_error(HF_EINVAL, "a cache overlaps an input");
   for (const Output &o : outputs)

@@ -149,23 +149,68 @@ struct Pool {
     each([](const Tensor &t) { written({&t}); });
   }
 };
-// what a caller gave for an output, or a new one in `made`
-template <size_t kN> void *output(PyObject *o, const char *name, at::ScalarType type, const int64_t (&shape)[kN], const Tensor &beside, Tensor &made) {
-  if (const Tensor *t = given(o, name)) return whole(t, name, type, shape, beside.get_device());
-  made = at::empty(at::IntArrayRef(shape, kN), beside.options().dtype(type));
-  return made.data_ptr();
-}
-PyObject *result(PyObject *o, Tensor &made) { return made.defined() ? wrap(std::move(made)) : again(o); }
-// `bytes` of workspace: the caller's or a new one
-template <typename A> void room_for(A &a, size_t bytes, PyObject *o, const Tensor &beside, Tensor &made) {
-  if (const Tensor *t = given(o, "workspace")) {
-    if (!t->is_cuda() || t->get_device() != beside.get_device() || !t->is_contiguous()) throw Wrong{"workspace", "a contiguous tensor on the operands' GPU is wanted"};
-    a.workspace = t->data_ptr(), a.workspace_bytes = t->nbytes();
-  } else {
-    made = at::empty({(int64_t)bytes}, beside.options().dtype(at::kByte));
-    a.workspace = made.data_ptr(), a.workspace_bytes = bytes;
+// The outputs of a call that its caller did not give, and a small workspace, in one allocation: the smallest calls wait for the host, which takes 0.65 us to allocate a tensor
+// (room for a token in 256 rows 7.3 -> 5.1 us a call).
+class Made {
+  static constexpr int64_t kSmall = 1 << 16; // a larger workspace does not stay with the outputs
+  struct One {
+    const char *name;
+    Tensor tensor;
+    at::ScalarType type;
+    c10::SmallVector<int64_t, 4> shape;
+    int64_t at;
+    void **to;
+  };
+  c10::SmallVector<One, 8> all_;
+  const Tensor &beside_;
+  int64_t size_ = 0;
+  Tensor store_, workspace_;
+  int64_t take(int64_t bytes) {
+    const int64_t at = size_;
+    size_ += (bytes + 15) / 16 * 16;
+    return at;
   }
-}
+
+public:
+  explicit Made(const Tensor &beside) : beside_(beside) {}
+  // `to` points to what the caller gave now, or to a new tensor of this type and shape after make(); returns the number of a new one, else -1
+  template <typename T> int output(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape, T **to) {
+    if (const Tensor *t = given(o, name)) {
+      if (!t->is_cuda() || t->get_device() != beside_.get_device()) throw Wrong{name, "a tensor on the operands' GPU is wanted"};
+      if (t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous()) throw Wrong{name, "a contiguous tensor of the output's type and shape is wanted"};
+      *to = static_cast<T *>(t->data_ptr());
+      return -1;
+    }
+    int64_t n = c10::elementSize(type);
+    for (const int64_t d : shape) n *= d;
+    all_.push_back({name, Tensor(), type, {shape.begin(), shape.end()}, take(n), reinterpret_cast<void **>(to)});
+    return (int)all_.size() - 1;
+  }
+  // and the workspace: the caller's, or a new one of `bytes`
+  template <typename A> void make(A &a, size_t bytes, PyObject *workspace) {
+    int64_t at = -1;
+    if (const Tensor *t = given(workspace, "workspace")) {
+      if (!t->is_cuda() || t->get_device() != beside_.get_device() || !t->is_contiguous()) throw Wrong{"workspace", "a contiguous tensor on the operands' GPU is wanted"};
+      a.workspace = t->data_ptr(), a.workspace_bytes = t->nbytes();
+    } else if ((int64_t)bytes <= kSmall) {
+      at = take((int64_t)bytes), a.workspace_bytes = bytes;
+    } else {
+      workspace_ = at::empty({(int64_t)bytes}, beside_.options().dtype(at::kByte));
+      a.workspace = workspace_.data_ptr(), a.workspace_bytes = bytes;
+    }
+    if (size_ == 0) return;
+    store_ = at::empty({size_}, beside_.options().dtype(at::kByte));
+    char *base = static_cast<char *>(store_.data_ptr());
+    if (at >= 0) a.workspace = base + at;
+    for (One &o : all_) {
+      o.tensor = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(store_.storage()), store_.key_set(), c10::scalarTypeToTypeMeta(o.type));
+      o.tensor.unsafeGetTensorImpl()->set_storage_offset(o.at / (int64_t)c10::elementSize(o.type));
+      o.tensor.unsafeGetTensorImpl()->set_sizes_contiguous(o.shape);
+      *o.to = base + o.at;
+    }
+  }
+  PyObject *result(int made, PyObject *o) { return made >= 0 ? wrap(std::move(all_[made].tensor)) : again(o); }
+};
 const Tensor &on_gpu(PyObject *o, const char *name) {
   const Tensor &t = wanted(o, name);
   if (!t.is_cuda()) throw Wrong{name, "a tensor on the GPU is wanted"};
@@ -193,17 +238,16 @@ PyObject *fork(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     a.lens = static_cast<const int32_t *>(whole(&wanted(arg[4], "lens"), "lens", at::kInt, {rows}, device));
     a.parents = static_cast<const int32_t *>(whole(&parents, "parents", at::kInt, {out}, device));
     a.refs = static_cast<const int32_t *>(whole(&wanted(arg[6], "refs"), "refs", at::kInt, {pool.pages()}, device));
-    Tensor new_tables, new_lens, new_refs, made_workspace;
-    a.tables_out = static_cast<int32_t *>(output(arg[7], "tables_out", at::kInt, {out, width}, tables, new_tables));
-    a.lens_out = static_cast<int32_t *>(output(arg[8], "lens_out", at::kInt, {out}, tables, new_lens));
-    a.refs_out = static_cast<int32_t *>(output(arg[9], "refs_out", at::kInt, {pool.pages()}, tables, new_refs));
+    Made made(tables);
+    const int new_tables = made.output(arg[7], "tables_out", at::kInt, {out, width}, &a.tables_out), new_lens = made.output(arg[8], "lens_out", at::kInt, {out}, &a.lens_out);
+    const int new_refs = made.output(arg[9], "refs_out", at::kInt, {pool.pages()}, &a.refs_out);
     const size_t size = hf_fork_pages_workspace_bytes(&pool.c, &a);
     if (size == (size_t)-1) return failed(HF_EINVAL, "hf_fork_pages_workspace_bytes");
-    room_for(a, size, arg[10], tables, made_workspace);
+    made.make(a, size, arg[10]);
     if (const int code = hf_fork_pages(&pool.c, &a, stream_of(arg[2]))) return failed(code, "hf_fork_pages");
     pool.moved();
     written({given(arg[7], "tables_out"), given(arg[8], "lens_out"), given(arg[9], "refs_out"), given(arg[10], "workspace")});
-    return tuple_of({result(arg[7], new_tables), result(arg[8], new_lens), result(arg[9], new_refs)});
+    return tuple_of({made.result(new_tables, arg[7]), made.result(new_lens, arg[8]), made.result(new_refs, arg[9])});
   });
 }
 
@@ -223,17 +267,15 @@ PyObject *grow(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     a.lens = static_cast<const int32_t *>(whole(&wanted(arg[4], "lens"), "lens", at::kInt, {rows}, device));
     a.counts = static_cast<const int32_t *>(whole(&wanted(arg[5], "counts"), "counts", at::kInt, {rows}, device));
     a.refs = static_cast<const int32_t *>(whole(&wanted(arg[6], "refs"), "refs", at::kInt, {pool.pages()}, device));
-    Tensor new_tables, new_lens, new_slots, new_refs, made_workspace;
-    a.tables_out = static_cast<int32_t *>(output(arg[8], "tables_out", at::kInt, {rows, width}, tables, new_tables));
-    a.lens_out = static_cast<int32_t *>(output(arg[9], "lens_out", at::kInt, {rows}, tables, new_lens));
-    a.slots = static_cast<int64_t *>(output(arg[10], "slots", at::kLong, {rows, most}, tables, new_slots));
-    a.refs_out = static_cast<int32_t *>(output(arg[11], "refs_out", at::kInt, {pool.pages()}, tables, new_refs));
+    Made made(tables);
+    const int new_tables = made.output(arg[8], "tables_out", at::kInt, {rows, width}, &a.tables_out), new_lens = made.output(arg[9], "lens_out", at::kInt, {rows}, &a.lens_out);
+    const int new_slots = made.output(arg[10], "slots", at::kLong, {rows, most}, &a.slots), new_refs = made.output(arg[11], "refs_out", at::kInt, {pool.pages()}, &a.refs_out);
     const size_t size = hf_grow_pages_workspace_bytes(&pool.c, &a);
     if (size == (size_t)-1) return failed(HF_EINVAL, "hf_grow_pages_workspace_bytes");
-    room_for(a, size, arg[12], tables, made_workspace);
+    made.make(a, size, arg[12]);
     if (const int code = hf_grow_pages(&pool.c, &a, stream_of(arg[2]))) return failed(code, "hf_grow_pages");
     written({given(arg[8], "tables_out"), given(arg[9], "lens_out"), given(arg[10], "slots"), given(arg[11], "refs_out"), given(arg[12], "workspace")});
-    return tuple_of({result(arg[8], new_tables), result(arg[9], new_lens), result(arg[10], new_slots), result(arg[11], new_refs)});
+    return tuple_of({made.result(new_tables, arg[8]), made.result(new_lens, arg[9]), made.result(new_slots, arg[10]), made.result(new_refs, arg[11])});
   });
 }
 
@@ -250,25 +292,20 @@ PyObject *compact(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     if (n > HF_MAX_TABLES) throw Wrong{"tables", "at most HF_MAX_TABLES at a time"};
     hf_page_compact a = {};
     a.refs = static_cast<const int32_t *>(whole(&refs, "refs", at::kInt, {pool.pages()}, device));
-    Tensor new_tables[HF_MAX_TABLES], new_refs, places, live, made_workspace;
+    Made made(refs);
+    int new_tables[HF_MAX_TABLES];
     for (Py_ssize_t i = 0; i < n; ++i) {
       const Tensor &t = on_gpu(PyTuple_GET_ITEM(arg[4], i), "tables");
-      const auto look = [&](const Tensor &x, const char *name) {
-        if (!x.is_cuda() || x.get_device() != device || x.scalar_type() != at::kInt || !x.is_contiguous() || x.sizes() != t.sizes()) throw Wrong{name, "contiguous int32 tensors on one GPU are wanted"};
-        return static_cast<int32_t *>(x.data_ptr());
-      };
-      a.entries[i] = look(t, "tables");
-      const Tensor *out = given(PyTuple_GET_ITEM(arg[5], i), "tables_out");
-      if (!out) new_tables[i] = at::empty(t.sizes(), t.options());
-      a.entries_out[i] = look(out ? *out : new_tables[i], "tables_out");
+      if (t.get_device() != device || t.scalar_type() != at::kInt || !t.is_contiguous()) throw Wrong{"tables", "contiguous int32 tensors on one GPU are wanted"};
+      a.entries[i] = static_cast<const int32_t *>(t.data_ptr());
       a.n_entries[i] = t.numel();
+      new_tables[i] = made.output(PyTuple_GET_ITEM(arg[5], i), "tables_out", at::kInt, t.sizes(), &a.entries_out[i]);
     }
-    a.refs_out = static_cast<int32_t *>(output(arg[6], "refs_out", at::kInt, {pool.pages()}, refs, new_refs));
-    places = at::empty({pool.pages()}, refs.options()), live = at::empty({}, refs.options());
-    a.places = static_cast<int32_t *>(places.data_ptr()), a.live = static_cast<int32_t *>(live.data_ptr());
+    const int new_refs = made.output(arg[6], "refs_out", at::kInt, {pool.pages()}, &a.refs_out);
+    const int places = made.output(Py_None, "places", at::kInt, {pool.pages()}, &a.places), live = made.output(Py_None, "live", at::kInt, {}, &a.live);
     const size_t size = hf_compact_pages_workspace_bytes(&pool.c, &a);
     if (size == (size_t)-1) return failed(HF_EINVAL, "hf_compact_pages_workspace_bytes");
-    room_for(a, size, arg[7], refs, made_workspace);
+    made.make(a, size, arg[7]);
     if (const int code = hf_compact_pages(&pool.c, &a, stream_of(arg[2]))) return failed(code, "hf_compact_pages");
     pool.moved();
     written({given(arg[6], "refs_out"), given(arg[7], "workspace")});
@@ -277,9 +314,9 @@ PyObject *compact(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     for (Py_ssize_t i = 0; i < n; ++i) {
       PyObject *o = PyTuple_GET_ITEM(arg[5], i);
       written({given(o, "tables_out")});
-      PyTuple_SET_ITEM(tables, i, result(o, new_tables[i]));
+      PyTuple_SET_ITEM(tables, i, made.result(new_tables[i], o));
     }
-    return tuple_of({tables, result(arg[6], new_refs), wrap(std::move(places)), wrap(std::move(live))});
+    return tuple_of({tables, made.result(new_refs, arg[6]), made.result(places, Py_None), made.result(live, Py_None)});
   });
 }
 
