@@ -661,7 +661,7 @@ HF_API int hf_adjust_logits(const hf_adjustment *args, void *hip_stream);
  * HF_DISTILL_REST the other tokens are one more: p_rest is their sum, q_rest = max(0, 1 - sum q_j), whose logarithm is taken as that of 2^-24 at least.
  *   loss = (1 - reverse) sum q (log q - log p)  +  reverse sum p (log p - log q)
  * A place of the list whose id is outside 0 .. vocab-1 or whose log probability is -inf names no token, and where an id comes twice its first place counts.  A row without any named
- * token is not read and has loss 0.  No rest is counted where no other token has p > 0 (all are named, or ruled out with -inf).  A named
+ * token has loss 0, whatever its logits are.  No rest is counted where no other token has p > 0 (all are named, or ruled out with -inf).  A named
  * token with x = -inf and q > 0 makes the loss inf if reverse < 1.  A row with NaN or +inf among its logits, or NaN among its log probabilities, has NaN results.
  * For hf_top_distill_back: norm holds the largest logit m of the tokens that are not named and log sum exp((x - m) * inv_temperature) over them, and
  * slopes the derivative of loss by the logit of every named token and, last, what exp((x_i - m) * inv_temperature - norm[1]) is multiplied by for every other.  One launch. */

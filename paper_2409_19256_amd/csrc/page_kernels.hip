@@ -556,7 +556,8 @@ __global__ __launch_bounds__(kSoloThreads) void grow_solo(Grow g) {
   int32_t have, want;
 #pragma unroll 2
   for (int i = t; i < g.from.rows * g.most; i += kSoloThreads) { // (the tables are read before they are written: they may be the same)
-    const int r = i / g.most, at = lens[r] + i % g.most, k = at >> shift;
+    const int r = i / g.most;
+    const int64_t at = (int64_t)lens[r] + i % g.most, k = at >> shift;
     int64_t slot = -1;
     if (grows(r, have, want) && i % g.most < counts[r]) {
       const int64_t p = k < have ? page_at(g.from, r, k) : list[before[r] + k - have];

@@ -167,7 +167,7 @@ def top_distill(logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch
     """How far every row of logits [rows, vocab] over the temperature is from a teacher known by log probabilities of some tokens, top_ids and top_logprobs
     [rows, places] (int32, float32; what token_logprobs(top=...) gives): (1 - reverse) KL(teacher || student) + reverse KL(student || teacher) over these
     tokens and, with rest, all others as one more.  Ids outside the vocabulary and log probabilities of -inf name nothing; rows without
-    a name are left out (loss 0).  Not differentiable by itself: see distill."""
+    a name have loss 0 and no gradient.  Not differentiable by itself: see distill."""
     return Distilled(*_steps.distill(_stream_of(_device_of(logits)), logits, top_ids, top_logprobs, temperature, reverse, rest))
 
 

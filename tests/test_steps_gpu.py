@@ -47,6 +47,9 @@ ADJUSTS = [
     ("bf16", 2, 50257, 0, 0, torch.int64, 0, 2),
     ("bf16", 2, 32000, 8, 0, torch.int64, 9, 0),
     ("f16", 66, 130, 0, 64, torch.int32, 4, 5),
+    ("bf16", 3, 9001, 0, 9000, torch.int64, 20, 2),  # more tokens than the lanes hold
+    ("f32", 17, 8192, 0, 5000, torch.int32, 70, 2),
+    ("f16", 2, 16385, 1, 40000, torch.int32, 700, 0),  # counts of 32 bits
 ]
 
 
@@ -243,15 +246,15 @@ def test_distill(case):
 @pytest.mark.gpu
 @pytest.mark.parametrize("rest", [True, False])
 @pytest.mark.parametrize("reverse", [0.0, 0.5, 1.0])
-@pytest.mark.parametrize("vocab", [53, 5004])
-def test_distill_lists(vocab, reverse, rest):
+@pytest.mark.parametrize("vocab,places", [(53, 30), (5004, 30), (5004, 200), (140001, 129)])
+def test_distill_lists(vocab, places, reverse, rest):
     """Places that name nothing, tokens that come twice, rows without a name."""
-    say("[distill, lists]", vocab, reverse, rest)
-    gen = gen_of(vocab, reverse, rest)
+    say("[distill, lists]", vocab, places, reverse, rest)
+    gen = gen_of(vocab, places, reverse, rest)
     x = logits_of(gen, 9, vocab, "f32", 1)
-    ids, lq = teacher(gen, x, 30)
+    ids, lq = teacher(gen, x, places)
     ids[0, ::3] = -1
-    ids[1, 1::2] = vocab + torch.arange(15, device="cuda").int()
+    ids[1, 1::2] = vocab + torch.arange(places // 2, device="cuda").int()
     lq[2, ::4] = -float("inf")
     ids[3, 5:9] = ids[3, 4]               # the first of five counts
     ids[4, 20], lq[4, 3] = ids[4, 3], -float("inf")  # a place without a log probability, and another with the same token
@@ -527,6 +530,73 @@ def test_more_pages_than_a_tile_of_each_workgroup():
 
 
 @pytest.mark.gpu
+def test_rows_that_share_a_page_that_is_not_full():
+    """Against the rule, by hand or by a cut length: the first that goes on in it has it, whoever it came from."""
+    say("[shared open page]")
+    gen = gen_of("shared")
+    pool = new_pool(gen, 2, 40, 2, 8, 16)
+    tables = torch.tensor([[3, 7, -1], [9, 7, 1], [3, 7, 5], [7, 7, 7]], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([13, 15, 20, 4], device="cuda", dtype=torch.int32)
+    refs = torch.zeros(40, device="cuda", dtype=torch.int32)
+    for p, n in ((3, 2), (7, 4), (9, 1), (5, 1), (0, 5)):
+        refs[p] = n
+    for parents in ([0, 1, 2, 3], [3, 1, 0, 0, 2, 2], [1, 1, 1], [2, 0]):
+        p = torch.tensor(parents, device="cuda", dtype=torch.int32)
+        want = S.fork(tables.cpu().numpy(), lens.cpu().numpy(), parents, refs.cpu().numpy(), 8)
+        before = images(pool)
+        t, n, r = pool.fork(tables, lens, p, refs)
+        same(t, want[0], "tables"), same(n, want[1], "lens"), same(r, want[2], "refs")
+        check_data(pool, before, want[3])
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """Pages and rows more than 2^32 elements from the first."""
+    from paper_2409_19256_amd import rollout
+    say("[offsets past 32 bits]")
+    gen = gen_of("far")
+    pages, page, dim = 280, 65536, 256  # 2^24 elements a page
+    pool = rollout.PagePool([rollout.KvCache.empty(pages, 1, page, dim)])
+    refs = torch.ones(pages, device="cuda", dtype=torch.int32)
+    refs[270], refs[275] = 0, 0
+    for t in pool._tensors:
+        t[260].normal_(generator=gen), t[270].zero_(), t[275].zero_(), t[0].zero_(), t[4].zero_()
+    tables, lens = torch.tensor([[260]], device="cuda", dtype=torch.int32), torch.tensor([40001], device="cuda", dtype=torch.int32)
+    t, n, r = pool.fork(tables, lens, torch.zeros(3, device="cuda", dtype=torch.int32), refs)
+    assert t.tolist() == [[260], [270], [275]] and n.tolist() == [40001] * 3
+    for x in pool._tensors:
+        for p in (270, 275):
+            assert torch.equal(x[p, :, :40001], x[260, :, :40001]) and not x[p, :, 40001:].any()
+        assert not x[4].any() and not x[0].any()  # 260 * 2^24 is 2^32 past page 4
+    r[0] = r[4] = 0
+    (t,), r, places, live = pool.compact(r, [t])
+    assert int(live) == 278 and places[278:].tolist() == [0, 4] and t.tolist() == [[260], [270], [275]]
+    del pool, x
+    torch.cuda.empty_cache()
+    far, vocab = (1 << 31) + 3, 5003
+    for dtype in ("bf16", "f32"):
+        store = torch.empty(2 * far + vocab, device="cuda", dtype=TYPES[dtype])
+        x = store.as_strided((3, vocab), (far, 1))
+        x.copy_(logits_of(gen, 3, vocab, dtype))
+        a = adjustment(dtype, 3, vocab, 0, 50, torch.int64, 5, 3, gen)
+        near_ = x.contiguous()
+        want = rollout.adjust_logits(near_, **a)
+        ids, lq = teacher(gen, near_, 9)
+        d = rollout.top_distill(near_, ids, lq)
+        g = torch.ones(3, device="cuda")
+        grad = rollout.top_distill_back(near_, ids, d.norm, d.slopes, g)
+        e = rollout.top_distill(x, ids, lq)
+        assert torch.equal(d.loss, e.loss) and torch.equal(rollout.top_distill_back(x, ids, e.norm, e.slopes, g), grad)
+        rollout.adjust_logits(x, **a, out=x)
+        assert torch.equal(bits_of(x), bits_of(want))
+        x.copy_(near_)
+        rollout.top_distill_back(x, ids, e.norm, e.slopes, g, out=x)
+        assert torch.equal(bits_of(x), bits_of(grad))
+        del store, x
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_caches_between_one_anothers_pages():
     """All layers in one allocation, a page of all of them in one piece."""
     from paper_2409_19256_amd.rollout import KvCache, PagePool
@@ -596,6 +666,42 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for k, (p, q) in enumerate(zip(captured, eager)):
             assert torch.equal(p, q) or torch.equal(p.isnan(), q.isnan()) and torch.equal(p.nan_to_num(), q.nan_to_num()), (i, k)
+
+
+@pytest.mark.gpu
+def test_autograd_in_a_graph():
+    """The loss and its gradient captured together, beside an eager graph over other leaves that lives on."""
+    from paper_2409_19256_amd import rollout
+    say("[graph, autograd]")
+    gen = gen_of("autograd")
+    x = logits_of(gen, 5, 999, "f32")
+    ids, lq = teacher(gen, x, 7)
+    w = torch.rand(5, generator=gen, device="cuda")
+    alive = x.clone().requires_grad_()
+    kept = rollout.distill(alive, ids, lq, 0.9, 0.2)
+
+    def step():
+        leaf = x.detach().requires_grad_()
+        loss = rollout.distill(leaf, ids, lq, 0.9, 0.2)
+        return loss.detach(), torch.autograd.grad((loss * w).sum(), leaf)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, grad = step()
+    for i in range(4):
+        x.copy_(logits_of(gen, 5, 999, "f32"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want[0]) and torch.equal(grad, want[1]), i
+    (kept * w).sum().backward()
+    assert torch.isfinite(alive.grad).all()
 
 
 @pytest.mark.gpu
