@@ -1,8 +1,10 @@
 // The pages of a model's caches: sequences that are dropped, go on or branch, room for new tokens, live pages moved to the lowest places.
 //
 // First the books, then the data.  The books are reference counts and page tables: counts are changed by atomics (whole numbers, in any order the same), and what has an
-// order (the f-th free page to the f-th row that wants one) comes from sums over tiles of pages and of rows, each tile's own in one launch and everybody's in the next.  The data are copied
-// by the same launch that writes the tables; they are bound by HBM, the books by the launches.
+// order (the f-th free page to the f-th row that wants one) comes from sums over the rows and pages in front: of small batches by one workgroup with the counts in shared memory,
+// else over tiles, each tile's own in one launch and everybody's in the next.  The books are bound by what follows one another (one workgroup 2.5-4.5 us, the launches 12-16).  The data are copied by the next
+// launch, which HBM bounds: 8 accesses of 16 bytes of a lane in flight, stores past the caches, the parts of a page on one XCD.  us of copying: a fork of 32 sequences into 128 in 160 buffers, 251 MB
+// written and 84 read, two thirds of them three times, 64 (5.2 TB/s); 245 pages of 512 KiB moved in four buffers, 1028 MB, 180 (5.7 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -121,6 +123,8 @@ template <> struct Access<8> { typedef uint32_t type __attribute__((ext_vector_t
 template <> struct Access<4> { typedef uint32_t type; };
 template <> struct Access<2> { typedef uint16_t type; };
 
+// us of fork / compact as above, with plain loads and non-temporal stores: 4 in flight 79 / 203, 8 70 / 205; plain stores 103 / 212 (4).  Loads past the caches: 125 / 196 (4), so that
+// compact, whose pages are read once, has them and fork does not.
 constexpr int kInFlight = 8;
 
 // Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.  kOnce: read past the caches.
