@@ -133,7 +133,7 @@ def fork(tables, lens, parents, refs, page):
         for i, p in enumerate(row):
             if p >= 0 and not (r in wants and i == len(row) - 1):
                 refs[p] += 1
-    free = [p for p in range(pages) if refs[p] == 0]
+    free = [p for p in range(pages) if refs[p] == 0 and p not in taken]  # (where counts are wrong, one that a row goes on in might have 0)
     copies = []
     for k, r in enumerate(wants):
         n, row = new[r]

@@ -530,6 +530,65 @@ def test_more_pages_than_a_tile_of_each_workgroup():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,width,pages", [(9, 4, 30), (300, 5, 900), (2100, 3, 9000), (40, 300, 2000)])
+def test_whatever_the_arrays_hold(rows, width, pages):
+    """Counts that fit no table, lengths below 0 and past the table, numbers that name no page: defined all the same, and nothing outside the caches is touched."""
+    say("[pages, anything]", rows, width, pages)
+    gen = gen_of("anything", rows, width, pages)
+    pool = new_pool(gen, 2, pages, 2, 4, 8)
+    rand = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=gen, device="cuda").int()  # noqa: E731
+    for _ in range(3):
+        tables, lens, refs = rand(-5, pages + 5, rows, width), rand(-9, 4 * width + 9, rows), rand(-2, 4, pages)
+        parents, counts = rand(-2, rows + 2, rows + 7), rand(-4, 12, rows)
+        want = S.fork(tables.cpu().numpy(), lens.cpu().numpy(), parents.cpu().numpy(), refs.cpu().numpy(), 4)
+        before = images(pool)
+        t, n, r = pool.fork(tables, lens, parents, refs)
+        same(t, want[0], "tables"), same(n, want[1], "lens"), same(r, want[2], "refs")
+        check_data(pool, before, want[3])
+        want = S.grow(tables.cpu().numpy(), lens.cpu().numpy(), counts.cpu().numpy(), refs.cpu().numpy(), 9, 4)
+        t, n, s, r = pool.grow(tables, lens, counts, refs, 9)
+        same(t, want[0], "tables"), same(n, want[1], "lens"), same(s, want[2], "slots"), same(r, want[3], "refs")
+        (new,), r_want, places, many, moves = S.compact(refs.cpu().numpy(), [tables.cpu().numpy()])
+        before = images(pool)
+        (t,), r, at, live = pool.compact(refs, [tables])
+        same(t, new, "tables"), same(r, r_want, "refs"), same(at, places, "places")
+        check_data(pool, before, [(a, b, 4) for a, b in moves])
+
+
+@pytest.mark.gpu
+def test_nothing_at_all():
+    """No rows, no width, no tokens, no tables."""
+    from paper_2409_19256_amd import rollout
+    say("[nothing]")
+    e = lambda *s, t=torch.int32: torch.empty(*s, device="cuda", dtype=t)  # noqa: E731
+    x = e(0, 50, t=torch.bfloat16)
+    assert rollout.adjust_logits(x, e(0, 9, t=torch.int64), e(0), repetition=e(0, t=torch.float32)).shape == (0, 50)
+    d = rollout.top_distill(x, e(0, 5), e(0, 5, t=torch.float32))
+    assert d.loss.shape == (0,) and d.norm.shape == (0, 2) and d.slopes.shape == (0, 6)
+    assert rollout.top_distill_back(x, e(0, 5), d.norm, d.slopes, e(0, t=torch.float32)).shape == (0, 50)
+    leaf = x.float().requires_grad_()
+    rollout.distill(leaf, e(0, 5), e(0, 5, t=torch.float32)).sum().backward()
+    assert leaf.grad.shape == (0, 50)
+    y = torch.randn(3, 50, device="cuda")
+    assert torch.equal(rollout.adjust_logits(y), y) and rollout.adjust_logits(y, out=y) is y
+    assert torch.equal(rollout.adjust_logits(y, e(3, 0, t=torch.int64), torch.zeros(3, device="cuda", dtype=torch.int32)), y)
+    assert torch.equal(rollout.adjust_logits(y, bias_ids=e(3, 0), bias=e(3, 0, t=torch.float32)), y)
+    pool = new_pool(gen_of("nothing"), 1, 5, 1, 4, 4)
+    before, refs = images(pool), torch.tensor([0, 2, 0, 1, 0], device="cuda", dtype=torch.int32)
+    for rows, out, width in ((0, 0, 0), (0, 3, 2), (2, 0, 0), (2, 3, 0)):
+        lens = torch.full((rows,), 7, device="cuda", dtype=torch.int32)
+        t, n, r = pool.fork(e(rows, width), lens, torch.zeros(out, device="cuda", dtype=torch.int32), refs)
+        assert t.shape == (out, width) and not n.any() and (t == -1).all() and torch.equal(r, refs)
+        t, n, s, r = pool.grow(e(rows, 0), lens, torch.ones(rows, device="cuda", dtype=torch.int32), refs, 2)
+        assert t.shape == (rows, 0) and not n.any() and s.shape == (rows, 2) and (s == -1).all() and torch.equal(r, refs)
+    tables, r, places, live = pool.compact(refs)
+    assert tables == () and r.tolist() == [1, 2, 0, 0, 0] and places.tolist() == [-1, 1, -1, 0, -1] and int(live) == 2
+    check_data(pool, before, [(3, 0, 4)])
+    (t,), r, _, _ = pool.compact(torch.zeros_like(refs), [e(0, 7)])
+    assert t.shape == (0, 7) and not r.any()
+
+
+@pytest.mark.gpu
 def test_rows_that_share_a_page_that_is_not_full():
     """Against the rule, by hand or by a cut length: the first that goes on in it has it, whoever it came from."""
     say("[shared open page]")

@@ -168,6 +168,17 @@ def test_caches_between_one_anothers_pages():
         assert (b"overlap" if meets else b"workspace") in B.hf_last_error(), moved
 
 
+@pytest.mark.parametrize("inside", ["heads", "tokens"])
+def test_caches_between_one_anothers_heads(inside):
+    """Four buffers whose heads, or tokens, take turns."""
+    stride = dict(heads=dict(head_stride=128, token_stride=8, page_stride=256), tokens=dict(head_stride=128, token_stride=32, page_stride=256))[inside]
+    step = 64 if inside == "heads" else 16  # bytes from one buffer's first to the next one's
+    at = [FAR + step * i for i in range(4)]
+    for moved, meets in ((0, False), (2, True), (-2, True)):
+        p = pool(cache(k=at[0], v=at[1], n_pages=50, **stride), cache(k=at[2] + moved, v=at[3], n_pages=50, **stride))
+        assert run_fork(fork(workspace=None), p) == B.HF_EINVAL and (b"overlap" if meets else b"workspace") in B.hf_last_error(), moved
+
+
 @pytest.mark.parametrize("bad", [
     dict(rows=-1), dict(rows_out=-1), dict(width=-1), dict(tables=None), dict(lens=None), dict(parents=None), dict(refs=None), dict(tables_out=None), dict(lens_out=None), dict(refs_out=None),
     dict(workspace=None), dict(workspace=20 * AT + 8), dict(workspace_bytes=8), dict(tables=AT + 2), dict(refs_out=9 * AT + 1)], ids=str)
