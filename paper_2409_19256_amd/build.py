@@ -6,6 +6,8 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -26,17 +28,25 @@ def hipcc() -> str:
 
 def build_library(verbose: bool = True) -> str:
     """Compile every source for gfx950 and link the shared library; returns its path.  rollout.py's native modules are built beside it where they can be."""
-    cmd = [hipcc(), "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared", "-fvisibility=hidden", "-Wl,-soname,libhfreshard.so",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           # kernel arguments arrive in registers: a workgroup here lives for two or three round trips to
-           # memory, and without this the first is for the arguments (small calls 2-6 % faster, long ones level)
-           "-mllvm", "-amdgpu-kernarg-preload-count=16",
-           "-Wall", "-Wno-unused-command-line-argument",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-DHF_BUILD",
-           "-x", "hip"] + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True, cwd=ROOT)
+    flags = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fvisibility=hidden",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             # kernel arguments arrive in registers: a workgroup here lives for two or three round trips to
+             # memory, and without this the first is for the arguments (small calls 2-6 % faster, long ones level)
+             "-mllvm", "-amdgpu-kernarg-preload-count=16",
+             "-Wall", "-Wno-unused-command-line-argument",
+             "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-DHF_BUILD"]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True, cwd=ROOT)
+
+    # a process for each source: one after another they take four minutes
+    with tempfile.TemporaryDirectory() as folder, ThreadPoolExecutor(int(os.environ.get("MAX_JOBS", 0)) or os.cpu_count() or 1) as jobs:
+        objects = [os.path.join(folder, s + ".o") for s in SOURCES]
+        for job in [jobs.submit(run, [hipcc()] + flags + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]:
+            job.result()
+        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-Wl,-soname,libhfreshard.so"] + objects + ["-o", LIB + ".tmp"])
     os.replace(LIB + ".tmp", LIB)
     # hfbench: native driver of the C ABI for rocprofv3 runs (no Python in the traced process)
     cmd = [hipcc(), "-O2", "-std=c++17", "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
