@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "step_kernels.hpp"
 
@@ -91,6 +92,7 @@ __device__ __forceinline__ i32x4 four_of(const int32_t *from, int64_t i, int64_t
     if (i + e < n) v[e] = from[i + e];
   return v;
 }
+
 // Tables of page numbers, and what of a row counts.
 struct Tables {
   const int32_t *entries, *lens;
@@ -721,7 +723,7 @@ int shift_of(int64_t n) { // n = 2^s
 Shape shape_of(const hf_kv_cache &c, int vec) {
   Shape s = {c.page_stride / vec, 0, 0, 1, 1, c.head_dim / vec, 1};
   const int64_t heads = c.n_kv_heads, dim = c.head_dim;
-  if (c.token_stride == dim || c.page_tokens == 1) { // a head's tokens in one run
+  if (c.token_stride == dim) { // a head's tokens in one run
     s.outer = (int32_t)heads, s.outer_stride = c.head_stride / vec, s.growing = 2;
   } else if (c.head_stride == dim || heads == 1) { // a token's heads in one run
     s.inner = (int32_t)(heads * dim / vec);
@@ -746,7 +748,7 @@ constexpr int64_t kSoloEntries = 8192;
 
 // arrays of a workspace, one after another, each 16-byte aligned
 struct Room {
-  char *at;
+  uintptr_t at;
   size_t size = 0;
   template <typename T> T *take(int64_t n) {
     T *p = reinterpret_cast<T *>(at + size);
@@ -803,24 +805,24 @@ template <typename F> hipError_t by_access(int vec, const F &go) {
 } // namespace
 
 size_t fork_workspace(const hf_page_pool &pool, const hf_page_fork &a) {
-  Room room = {nullptr};
+  Room room = {0};
   fork_of(pool, a, room);
   return room.size;
 }
 size_t grow_workspace(const hf_page_pool &pool, const hf_page_grow &a) {
-  Room room = {nullptr};
+  Room room = {0};
   grow_of(pool, a, room);
   return room.size;
 }
 size_t compact_workspace(const hf_page_pool &pool, const hf_page_compact &a) {
-  Room room = {nullptr};
+  Room room = {0};
   compact_of(pool, a, room);
   return room.size;
 }
 
 int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Room room = {static_cast<char *>(a.workspace)};
+  Room room = {reinterpret_cast<uintptr_t>(a.workspace)};
   const Fork f = fork_of(pool, a, room);
   const auto wgs = [](int64_t n, int64_t each) { return dim3((uint32_t)std::max<int64_t>(1, std::min(up(n, each), kMostRowWgs))); };
   const bool solo = f.from.n_pages <= kSoloPages && std::max(a.rows, a.rows_out) <= kSoloRows && (int64_t)std::max(a.rows, a.rows_out) * a.width <= kSoloEntries;
@@ -842,7 +844,7 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *
 
 int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Room room = {static_cast<char *>(a.workspace)};
+  Room room = {reinterpret_cast<uintptr_t>(a.workspace)};
   const Grow g = grow_of(pool, a, room);
   if (g.from.n_pages <= kSoloPages && a.rows <= kSoloRows && g.list <= kSoloFresh && (int64_t)a.rows * ((int64_t)a.width + a.most) <= 2 * kSoloEntries)
     return enqueue_kernel(grow_solo, dim3(1), kSoloThreads, st, g);
@@ -853,7 +855,7 @@ int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
 
 int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, int vec, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Room room = {static_cast<char *>(a.workspace)};
+  Room room = {reinterpret_cast<uintptr_t>(a.workspace)};
   const Compact c = compact_of(pool, a, room);
   if (c.n_pages <= kSoloPages) {
     if (const hipError_t e = enqueue_kernel(compact_solo, dim3(1), kSoloThreads, st, c)) return e;

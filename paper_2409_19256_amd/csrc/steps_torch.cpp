@@ -22,6 +22,72 @@ void *like(const Tensor &t, const Tensor &logits) {
   return t.data_ptr();
 }
 
+// The outputs of a call that its caller did not give, and a small workspace, in one allocation: the smallest calls wait for the host, which takes 0.65 us to allocate a tensor
+// (room for a token in 256 rows 7.3 -> 4.9 us a call).
+class Made {
+  static constexpr int64_t kSmall = 1 << 16; // a larger workspace does not stay with the outputs
+  struct One {
+    const char *name;
+    Tensor tensor;
+    at::ScalarType type;
+    c10::SmallVector<int64_t, 4> shape;
+    int64_t at;
+    void **to;
+  };
+  c10::SmallVector<One, 8> all_;
+  const Tensor &beside_;
+  int64_t size_ = 0;
+  Tensor store_, workspace_;
+  int64_t take(int64_t bytes) {
+    const int64_t at = size_;
+    size_ += (bytes + 15) / 16 * 16;
+    return at;
+  }
+
+public:
+  explicit Made(const Tensor &beside) : beside_(beside) {}
+  // `to` points to what the caller gave now, or to a new tensor of this type and shape after make(); returns the number of a new one, else -1
+  template <typename T> int output(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape, T **to) {
+    if (const Tensor *t = given(o, name)) {
+      if (!t->is_cuda() || t->get_device() != beside_.get_device()) throw Wrong{name, "a tensor on the operands' GPU is wanted"};
+      if (t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous()) throw Wrong{name, "a contiguous tensor of the output's type and shape is wanted"};
+      *to = static_cast<T *>(t->data_ptr());
+      return -1;
+    }
+    int64_t n = c10::elementSize(type);
+    for (const int64_t d : shape) n *= d;
+    all_.push_back({name, Tensor(), type, {shape.begin(), shape.end()}, take(n), reinterpret_cast<void **>(to)});
+    return (int)all_.size() - 1;
+  }
+  // and the workspace: the caller's, or a new one of `bytes`
+  template <typename A> void make(A &a, size_t bytes, PyObject *workspace) {
+    int64_t at = -1;
+    if (const Tensor *t = given(workspace, "workspace")) {
+      if (!t->is_cuda() || t->get_device() != beside_.get_device() || !t->is_contiguous()) throw Wrong{"workspace", "a contiguous tensor on the operands' GPU is wanted"};
+      a.workspace = t->data_ptr(), a.workspace_bytes = t->nbytes();
+    } else if ((int64_t)bytes <= kSmall) {
+      at = take((int64_t)bytes), a.workspace_bytes = bytes;
+    } else {
+      workspace_ = at::empty({(int64_t)bytes}, beside_.options().dtype(at::kByte));
+      a.workspace = workspace_.data_ptr(), a.workspace_bytes = bytes;
+    }
+    make();
+    if (at >= 0) a.workspace = static_cast<char *>(store_.data_ptr()) + at;
+  }
+  void make() {
+    if (all_.empty() && size_ == 0) return;
+    store_ = at::empty({size_ ? size_ : 16}, beside_.options().dtype(at::kByte));
+    char *base = static_cast<char *>(store_.data_ptr());
+    for (One &o : all_) {
+      o.tensor = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(store_.storage()), store_.key_set(), c10::scalarTypeToTypeMeta(o.type));
+      o.tensor.unsafeGetTensorImpl()->set_storage_offset(o.at / (int64_t)c10::elementSize(o.type));
+      o.tensor.unsafeGetTensorImpl()->set_sizes_contiguous(o.shape);
+      *o.to = base + o.at;
+    }
+  }
+  PyObject *result(int made, PyObject *o) { return made >= 0 ? wrap(std::move(all_[made].tensor)) : again(o); }
+};
+
 // (stream, logits, tokens, lens, prompt_lens, repetition, frequency, presence, bias_ids, bias, allowed, allowed_rows, out) -> out
 PyObject *adjust(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
   return guarded(n_args, 13, [&]() -> PyObject * {
@@ -89,11 +155,12 @@ PyObject *distill(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     const int rest = PyObject_IsTrue(arg[6]);
     if (rest < 0) throw python_error();
     a.flags = rest ? HF_DISTILL_REST : 0;
-    const auto options = logits.options().dtype(at::kFloat);
-    Tensor loss = at::empty({x.rows}, options), norm = at::empty({x.rows, 2}, options), slopes = at::empty({x.rows, n + 1}, options);
-    a.loss = static_cast<float *>(loss.data_ptr()), a.norm = static_cast<float *>(norm.data_ptr()), a.slopes = static_cast<float *>(slopes.data_ptr());
+    Made made(logits);
+    const int loss = made.output(Py_None, "loss", at::kFloat, {x.rows}, &a.loss), norm = made.output(Py_None, "norm", at::kFloat, {x.rows, 2}, &a.norm);
+    const int slopes = made.output(Py_None, "slopes", at::kFloat, {x.rows, n + 1}, &a.slopes);
+    made.make();
     if (const int code = hf_top_distill(&x, &a, stream_of(arg[0]))) return failed(code, "hf_top_distill");
-    return tuple_of({wrap(std::move(loss)), wrap(std::move(norm)), wrap(std::move(slopes))});
+    return tuple_of({made.result(loss, Py_None), made.result(norm, Py_None), made.result(slopes, Py_None)});
   });
 }
 
@@ -148,68 +215,6 @@ struct Pool {
   void moved() const {
     each([](const Tensor &t) { written({&t}); });
   }
-};
-// The outputs of a call that its caller did not give, and a small workspace, in one allocation: the smallest calls wait for the host, which takes 0.65 us to allocate a tensor
-// (room for a token in 256 rows 7.3 -> 5.1 us a call).
-class Made {
-  static constexpr int64_t kSmall = 1 << 16; // a larger workspace does not stay with the outputs
-  struct One {
-    const char *name;
-    Tensor tensor;
-    at::ScalarType type;
-    c10::SmallVector<int64_t, 4> shape;
-    int64_t at;
-    void **to;
-  };
-  c10::SmallVector<One, 8> all_;
-  const Tensor &beside_;
-  int64_t size_ = 0;
-  Tensor store_, workspace_;
-  int64_t take(int64_t bytes) {
-    const int64_t at = size_;
-    size_ += (bytes + 15) / 16 * 16;
-    return at;
-  }
-
-public:
-  explicit Made(const Tensor &beside) : beside_(beside) {}
-  // `to` points to what the caller gave now, or to a new tensor of this type and shape after make(); returns the number of a new one, else -1
-  template <typename T> int output(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape, T **to) {
-    if (const Tensor *t = given(o, name)) {
-      if (!t->is_cuda() || t->get_device() != beside_.get_device()) throw Wrong{name, "a tensor on the operands' GPU is wanted"};
-      if (t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous()) throw Wrong{name, "a contiguous tensor of the output's type and shape is wanted"};
-      *to = static_cast<T *>(t->data_ptr());
-      return -1;
-    }
-    int64_t n = c10::elementSize(type);
-    for (const int64_t d : shape) n *= d;
-    all_.push_back({name, Tensor(), type, {shape.begin(), shape.end()}, take(n), reinterpret_cast<void **>(to)});
-    return (int)all_.size() - 1;
-  }
-  // and the workspace: the caller's, or a new one of `bytes`
-  template <typename A> void make(A &a, size_t bytes, PyObject *workspace) {
-    int64_t at = -1;
-    if (const Tensor *t = given(workspace, "workspace")) {
-      if (!t->is_cuda() || t->get_device() != beside_.get_device() || !t->is_contiguous()) throw Wrong{"workspace", "a contiguous tensor on the operands' GPU is wanted"};
-      a.workspace = t->data_ptr(), a.workspace_bytes = t->nbytes();
-    } else if ((int64_t)bytes <= kSmall) {
-      at = take((int64_t)bytes), a.workspace_bytes = bytes;
-    } else {
-      workspace_ = at::empty({(int64_t)bytes}, beside_.options().dtype(at::kByte));
-      a.workspace = workspace_.data_ptr(), a.workspace_bytes = bytes;
-    }
-    if (size_ == 0) return;
-    store_ = at::empty({size_}, beside_.options().dtype(at::kByte));
-    char *base = static_cast<char *>(store_.data_ptr());
-    if (at >= 0) a.workspace = base + at;
-    for (One &o : all_) {
-      o.tensor = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(store_.storage()), store_.key_set(), c10::scalarTypeToTypeMeta(o.type));
-      o.tensor.unsafeGetTensorImpl()->set_storage_offset(o.at / (int64_t)c10::elementSize(o.type));
-      o.tensor.unsafeGetTensorImpl()->set_sizes_contiguous(o.shape);
-      *o.to = base + o.at;
-    }
-  }
-  PyObject *result(int made, PyObject *o) { return made >= 0 ? wrap(std::move(all_[made].tensor)) : again(o); }
 };
 const Tensor &on_gpu(PyObject *o, const char *name) {
   const Tensor &t = wanted(o, name);
