@@ -75,7 +75,7 @@ public:
     if (at >= 0) a.workspace = static_cast<char *>(store_.data_ptr()) + at;
   }
   void make() {
-    if (all_.empty() && size_ == 0) return;
+    if (all_.size() == 0 && size_ == 0) return;
     store_ = at::empty({size_ ? size_ : 16}, beside_.options().dtype(at::kByte));
     char *base = static_cast<char *>(store_.data_ptr());
     for (One &o : all_) {
