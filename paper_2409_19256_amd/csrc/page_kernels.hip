@@ -108,9 +108,9 @@ __device__ __forceinline__ int32_t page_at(const Tables &t, int64_t row, int64_t
 
 // ---- the data ------------------------------------------------------------------------------------------------------------
 
-// How the tokens of a page lie in a cache, in accesses: runs of `inner`, of which there are outer * middle.  One of the three grows with the number of tokens.
+// How the tokens of a page lie in a cache, in elements: runs of `inner`, of which there are outer * middle.  One of the three grows with the number of tokens.
 struct Shape {
-  int64_t page, outer_stride, middle_stride; // in accesses
+  int64_t page, outer_stride, middle_stride;
   int32_t outer, middle, inner;
   int32_t growing; // 0: outer, 1: middle, 2: inner
 };
@@ -119,38 +119,42 @@ struct Buffers {
   int32_t n;
 };
 
-template <int kVecBytes> struct Access;
-template <> struct Access<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Access<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
-template <> struct Access<4> { typedef uint32_t type; };
-template <> struct Access<2> { typedef uint16_t type; };
+// A run of at least 8 elements is copied 8 at a time wherever it begins, the last ones of it ending where it ends: what two of them have in common is written twice, alike.
+// Three heads of 65 in pages of 32, half of 1580 pages live, five layers: 22.9 us where single elements took 52.6; heads of 72 and 128 level with accesses that know their alignment.
+template <int kVec> struct Access {
+  typedef uint16_t type __attribute__((ext_vector_type(kVec)));
+  typedef type any __attribute__((aligned(2)));
+};
+template <> struct Access<1> {
+  typedef uint16_t type, any;
+};
 
 // us of fork / compact as above, with plain loads and non-temporal stores: 4 in flight 79 / 203, 8 70 / 205; plain stores 103 / 212 (4).  Loads past the caches: 125 / 196 (4), so that
 // compact, whose pages are read once, has them and fork does not.
 constexpr int kInFlight = 8;
 
 // Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.  kOnce: read past the caches.
-template <int kVecBytes, bool kOnce> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, uint32_t part) {
-  typedef typename Access<kVecBytes>::type V;
+template <int kVec, bool kOnce> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, uint32_t part) {
+  typedef typename Access<kVec>::any V;
   const uint32_t outer = s.growing == 0 ? tokens : s.outer, middle = s.growing == 1 ? tokens : s.middle, inner = s.growing == 2 ? s.inner * tokens : s.inner;
-  const uint32_t n = outer * middle * inner; // (fits: a page has fewer than 2^31 elements)
-  V *base = static_cast<V *>(buffer);
+  const uint32_t each = (inner + kVec - 1) / kVec, n = outer * middle * each; // (fits: a page has fewer than 2^31 elements)
+  uint16_t *base = static_cast<uint16_t *>(buffer);
   uint32_t at = part * (kThreads * kInFlight) + threadIdx.x;
   int64_t off[kInFlight];
-  V v[kInFlight];
+  typename Access<kVec>::type v[kInFlight];
 #pragma unroll
   for (int k = 0; k < kInFlight; ++k, at += kThreads) {
     if (at >= n) break;
-    const uint32_t run = at / inner, x = at % inner;
+    const uint32_t run = at / each, x = min(at % each * kVec, inner - kVec);
     off[k] = s.growing == 1 ? run / middle * s.outer_stride + run % middle * s.middle_stride + x : run * s.outer_stride + x;
-    const V *from = base + (src * s.page + off[k]);
+    const V *from = reinterpret_cast<const V *>(base + (src * s.page + off[k]));
     v[k] = kOnce ? __builtin_nontemporal_load(from) : *from;
   }
   at = part * (kThreads * kInFlight) + threadIdx.x;
 #pragma unroll
   for (int k = 0; k < kInFlight; ++k, at += kThreads) {
     if (at >= n) break;
-    __builtin_nontemporal_store(v[k], base + (dst * s.page + off[k]));
+    __builtin_nontemporal_store(v[k], reinterpret_cast<V *>(base + (dst * s.page + off[k])));
   }
 }
 
@@ -301,11 +305,11 @@ __device__ __forceinline__ void fork_rows(const Fork &f, int64_t wave, int64_t w
   }
 }
 // row_wgs: workgroups that write tables, a wavefront to a row; the others copy
-template <int kVecBytes> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, uint32_t row_wgs, uint32_t parts) {
+template <int kVec> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, uint32_t row_wgs, uint32_t parts) {
   if (blockIdx.x < row_wgs) return fork_rows(f, blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave, (int64_t)row_wgs * kWaves);
   each_part(min(f.totals[0], f.totals[1]), buffers.n, parts, blockIdx.x - row_wgs, gridDim.x - row_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
     const Move m = f.moves[k];
-    copy_part<kVecBytes, false>(buffers.at[b], shape, m.from, f.free_list[k], m.tokens, part); // (several may copy one page)
+    copy_part<kVec, false>(buffers.at[b], shape, m.from, f.free_list[k], m.tokens, part); // (several may copy one page)
   });
 }
 
@@ -698,7 +702,7 @@ __global__ __launch_bounds__(kSoloThreads) void compact_solo(Compact c) {
   if (t == 0) c.totals[0] = live - stay, *c.live = live;
 }
 // entry_wgs: workgroups that rewrite tables; the others copy
-template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, uint32_t entry_wgs, uint32_t parts) {
+template <int kVec> __global__ __launch_bounds__(kThreads) void compact_apply(Compact c, Buffers buffers, Shape shape, int32_t page_tokens, uint32_t entry_wgs, uint32_t parts) {
   if (blockIdx.x < entry_wgs) {
     for (int k = 0; k < HF_MAX_TABLES; ++k)
       for (int64_t i = blockIdx.x * (int64_t)kThreads + threadIdx.x; i < c.n_entries[k]; i += (int64_t)entry_wgs * kThreads) {
@@ -708,7 +712,7 @@ template <int kVecBytes> __global__ __launch_bounds__(kThreads) void compact_app
     return;
   }
   each_part(c.totals[0], buffers.n, parts, blockIdx.x - entry_wgs, gridDim.x - entry_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
-    copy_part<kVecBytes, true>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
+    copy_part<kVec, true>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
   });
 }
 
@@ -720,17 +724,17 @@ int shift_of(int64_t n) { // n = 2^s
   return s;
 }
 
-Shape shape_of(const hf_kv_cache &c, int vec) {
-  Shape s = {c.page_stride / vec, 0, 0, 1, 1, c.head_dim / vec, 1};
+Shape shape_of(const hf_kv_cache &c) {
+  Shape s = {c.page_stride, 0, 0, 1, 1, c.head_dim, 1};
   const int64_t heads = c.n_kv_heads, dim = c.head_dim;
   if (c.token_stride == dim) { // a head's tokens in one run
-    s.outer = (int32_t)heads, s.outer_stride = c.head_stride / vec, s.growing = 2;
+    s.outer = (int32_t)heads, s.outer_stride = c.head_stride, s.growing = 2;
   } else if (c.head_stride == dim || heads == 1) { // a token's heads in one run
-    s.inner = (int32_t)(heads * dim / vec);
+    s.inner = (int32_t)(heads * dim);
     if (c.token_stride == heads * dim) s.growing = 2;
-    else s.growing = 0, s.outer_stride = c.token_stride / vec;
+    else s.growing = 0, s.outer_stride = c.token_stride;
   } else {
-    s.outer = (int32_t)heads, s.outer_stride = c.head_stride / vec, s.middle_stride = c.token_stride / vec, s.growing = 1;
+    s.outer = (int32_t)heads, s.outer_stride = c.head_stride, s.middle_stride = c.token_stride, s.growing = 1;
   }
   return s;
 }
@@ -739,7 +743,13 @@ Buffers buffers_of(const hf_page_pool &pool) {
   for (int i = 0; i < pool.n_caches; ++i) b.at[b.n++] = pool.caches[i].k, b.at[b.n++] = pool.caches[i].v;
   return b;
 }
-uint32_t parts_of(const hf_kv_cache &c, int vec) { return (uint32_t)up((int64_t)c.n_kv_heads * c.page_tokens * c.head_dim / vec, kThreads * kInFlight); }
+// f(elements of an access, workgroups' shares of a whole page): 8 at a time where the shortest run has as many
+template <typename F> hipError_t by_access(const Shape &s, int32_t page_tokens, const F &f) {
+  const int vec = s.inner >= 8 ? 8 : 1;
+  const int64_t runs = (int64_t)s.outer * s.middle * (s.growing < 2 ? page_tokens : 1), inner = s.growing == 2 ? (int64_t)s.inner * page_tokens : s.inner;
+  const uint32_t parts = (uint32_t)up(runs * up(inner, vec), kThreads * kInFlight);
+  return vec == 8 ? f(std::integral_constant<int, 8>{}, parts) : f(std::integral_constant<int, 1>{}, parts);
+}
 constexpr int64_t kMostCopyWgs = 16384, kMostRowWgs = 2048;
 // One workgroup keeps the books of up to kSoloPages pages and kSoloEntries entries of tables (of tables and slots, twice as many): us, by one / by launches after one another, fork of 256 rows of 8, 31
 // and 60 pages 8.8 / 16.1, 16.0 / 17.3, 25.5 / 17.8; grow by one token of 256 rows in 4096 and 16384 pages 8.0 / 10.2, 15.1 / 10.8, by 900 of 16 rows 10.5 / 12.6; compact of 1024, 8192 and 16384 pages
@@ -798,10 +808,6 @@ Compact compact_of(const hf_page_pool &pool, const hf_page_compact &a, Room &roo
   return c;
 }
 
-template <typename F> hipError_t by_access(int vec, const F &go) {
-  return vec == 8 ? go(std::integral_constant<int, 16>{}) : vec == 4 ? go(std::integral_constant<int, 8>{}) : vec == 2 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
-}
-
 } // namespace
 
 size_t fork_workspace(const hf_page_pool &pool, const hf_page_fork &a) {
@@ -820,7 +826,7 @@ size_t compact_workspace(const hf_page_pool &pool, const hf_page_compact &a) {
   return room.size;
 }
 
-int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *stream) {
+int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   Room room = {reinterpret_cast<uintptr_t>(a.workspace)};
   const Fork f = fork_of(pool, a, room);
@@ -834,11 +840,12 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, int vec, void *
     if (const hipError_t e = enqueue_kernel(fork_sums, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
     if (const hipError_t e = enqueue_kernel(fork_lists, dim3(f.page_tiles + f.row_tiles), kThreads, st, f)) return e;
   }
-  const uint32_t parts = parts_of(pool.caches[0], vec), row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
-  const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
-  if (row_wgs + copies == 0) return hipSuccess;
-  return by_access(vec, [&](auto bytes) {
-    return enqueue_kernel(fork_apply<decltype(bytes)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape_of(pool.caches[0], vec), row_wgs, parts);
+  const uint32_t row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
+  const Shape shape = shape_of(pool.caches[0]);
+  return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
+    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
+    if (row_wgs + copies == 0) return hipSuccess;
+    return enqueue_kernel(fork_apply<decltype(vec)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape, row_wgs, parts);
   });
 }
 
@@ -853,7 +860,7 @@ int launch_grow(const hf_page_pool &pool, const hf_page_grow &a, void *stream) {
   return enqueue_kernel(grow_apply, dim3((uint32_t)std::max<int64_t>(1, std::min(up(a.rows, kWaves), kMostRowWgs))), kThreads, st, g);
 }
 
-int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, int vec, void *stream) {
+int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   Room room = {reinterpret_cast<uintptr_t>(a.workspace)};
   const Compact c = compact_of(pool, a, room);
@@ -866,12 +873,12 @@ int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, int vec, 
   }
   int64_t most = 0;
   for (const int64_t n : c.n_entries) most = std::max(most, n);
-  const uint32_t parts = parts_of(pool.caches[0], vec), entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
-  const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
-  if (entry_wgs + copies == 0) return hipSuccess;
-  return by_access(vec, [&](auto bytes) {
-    return enqueue_kernel(compact_apply<decltype(bytes)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape_of(pool.caches[0], vec),
-                          pool.caches[0].page_tokens, entry_wgs, parts);
+  const uint32_t entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
+  const Shape shape = shape_of(pool.caches[0]);
+  return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
+    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
+    if (entry_wgs + copies == 0) return hipSuccess;
+    return enqueue_kernel(compact_apply<decltype(vec)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape, pool.caches[0].page_tokens, entry_wgs, parts);
   });
 }
 

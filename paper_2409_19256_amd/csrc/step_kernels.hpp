@@ -18,12 +18,11 @@ int launch_top_distill_back(const hf_logits &in, const hf_distillation_grad &gra
 // workgroups per row of top_distill_back
 uint32_t distill_back_segments(const hf_logits &in);
 
-// elements per access when pages are copied: the widest (8, 4, 2, 1) that divides the head, every stride and address
 size_t fork_workspace(const hf_page_pool &pool, const hf_page_fork &args);
 size_t grow_workspace(const hf_page_pool &pool, const hf_page_grow &args);
 size_t compact_workspace(const hf_page_pool &pool, const hf_page_compact &args);
-int launch_fork(const hf_page_pool &pool, const hf_page_fork &args, int vec, void *stream);
+int launch_fork(const hf_page_pool &pool, const hf_page_fork &args, void *stream);
 int launch_grow(const hf_page_pool &pool, const hf_page_grow &args, void *stream);
-int launch_compact(const hf_page_pool &pool, const hf_page_compact &args, int vec, void *stream);
+int launch_compact(const hf_page_pool &pool, const hf_page_compact &args, void *stream);
 
 } // namespace hf

@@ -121,18 +121,6 @@ public:
   }
 };
 
-int access_of(const hf_page_pool &pool) {
-  const hf_kv_cache &c = pool.caches[0];
-  const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
-  int vec = 8;
-  for (; vec > 1; vec /= 2) {
-    bool fits = c.head_dim % vec == 0;
-    for (const Dim &d : dims) fits = fits && (d.n <= 1 || d.stride % vec == 0);
-    for (int i = 0; fits && i < pool.n_caches; ++i) fits = aligned(pool.caches[i].k, 2 * vec) && aligned(pool.caches[i].v, 2 * vec);
-    if (fits) break;
-  }
-  return vec;
-}
 // a page in one buffer has to be countable in 32 bits
 int check_moves(const hf_page_pool &pool) {
   const hf_kv_cache &c = pool.caches[0];
@@ -257,7 +245,7 @@ int hf_fork_pages(const hf_page_pool *pool, const hf_page_fork *args, void *hip_
     if (buffers.meet(o.place)) return set_error(HF_EINVAL, "a cache overlaps an output");
   if (buffers.meet_one_another()) return set_error(HF_EINVAL, "the caches overlap one another");
   if (int rc = check_workspace(a.workspace, a.workspace_bytes, need)) return rc;
-  return launched(hf::launch_fork(*pool, a, access_of(*pool), hip_stream));
+  return launched(hf::launch_fork(*pool, a, hip_stream));
 }
 
 size_t hf_grow_pages_workspace_bytes(const hf_page_pool *pool, const hf_page_grow *args) {
@@ -328,7 +316,7 @@ int hf_compact_pages(const hf_page_pool *pool, const hf_page_compact *args, void
     if (buffers.meet(o.place)) return set_error(HF_EINVAL, "a cache overlaps an output");
   if (buffers.meet_one_another()) return set_error(HF_EINVAL, "the caches overlap one another");
   if (int rc = check_workspace(a.workspace, a.workspace_bytes, need)) return rc;
-  return launched(hf::launch_compact(*pool, a, access_of(*pool), hip_stream));
+  return launched(hf::launch_compact(*pool, a, hip_stream));
 }
 
 } // extern "C"
