@@ -637,7 +637,7 @@ HF_API int hf_token_logprobs_back(const hf_logits *in, const hf_logprobs_grad *g
  * nothing applies to keep their bits. */
 typedef struct {
   const void *logits;         /* [rows, vocab] of dtype */
-  void *out;                  /* the same shape and type; may be the logits, with the same stride: of rows without a mask then only what changes is written */
+  void *out;                  /* the same shape and type; may be the logits, with the same stride: rows without a mask and with few tokens are then not moved */
   const void *tokens;         /* [rows, width] of int32 or int64; may be null */
   const int32_t *lens;        /* [rows]; null exactly if tokens is */
   const int32_t *prompt_lens; /* [rows]; null: no prompts */

@@ -5,7 +5,7 @@
 // Every logit is read once and written once, so HBM is the bound.  A workgroup takes a piece of a row: it asks for its logits, counts the row's tokens that
 // fall into the piece in shared memory while they are on their way, lays them there, changes those that were counted or have a bias, each by one lane (whose bias
 // is the token's last, or who is first to take the count away), and writes the piece.  The work beside the copy goes by the tokens and biases, not by the logits: a look at
-// every logit's count took more than HBM leaves room for.  In place and without a mask nothing is moved but what changes.
+// every logit's count took more than HBM leaves room for.  In place, of rows without a mask and with few tokens, nothing is moved but what changes.
 //
 // us, out of place, beside the copy alone by the same workgroups: 1024 x 32000 bf16, 900 tokens a row, half of the rows masked 24.2 beside 22.0; 1024 x 128256 f32, 2800 tokens and 64 biases a row,
 // half masked 208 beside 170-189 (5.1 TB/s); 64 x 32000 bf16 4.8, one workgroup after another's data (lengths, tokens, counts, logits).  Pieces of 4096 / 8192 / 16384 (256 / 512 / 1024 lanes)
@@ -77,7 +77,10 @@ template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __gl
     const int64_t g = a.allowed_rows ? a.allowed_rows[r] : r;
     if (g >= 0 && g < a.n_allowed) allowed = reinterpret_cast<const uint8_t *>(a.allowed + g * a.allowed_stride) + begin / 8;
   }
-  const bool sparse = from == to && !allowed; // nothing is moved but what changes
+  const int n = kTables && a.tokens ? min(max(a.lens[r], 0), a.width) : 0;
+  // In place, without a mask and with few tokens nothing is moved but what changes.  us, by the token / by the piece, 1024 rows of 32000 bf16 with 64, 1024 and 4096 tokens 13.0 / 21.3, 20.4 / 23.8, 49.8 / 36.6,
+  // 1024 of 128256 f32 45 / 184, 72 / 194, 240 / 203: a token costs as much as some 40 logits.
+  const bool sparse = from == to && !allowed && n + (int64_t)a.n_bias <= a.vocab / 40;
   if (!kTables && sparse) return;
   const int n_last = sparse ? 0 : min(kV, size - n_vec * kV); // elements past the whole vectors, a lane each
 
@@ -94,7 +97,7 @@ template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __gl
     }
   }
   if constexpr (kTables) {
-    const int n = a.tokens ? min(max(a.lens[r], 0), a.width) : 0, prompt = a.prompt_lens ? a.prompt_lens[r] : 0;
+    const int prompt = a.prompt_lens ? a.prompt_lens[r] : 0;
     const Row row = {a.repetition ? a.repetition[r] : 1.f, a.frequency ? a.frequency[r] : 0.f, a.presence ? a.presence[r] : 0.f};
     const Token *tokens = static_cast<const Token *>(a.tokens) + r * a.tokens_stride;
     Token held[kHeld];

@@ -133,30 +133,37 @@ template <> struct Access<1> {
 // compact, whose pages are read once, has them and fork does not.
 constexpr int kInFlight = 8;
 
-// Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of page `src`, to page `dst`.  kOnce: read past the caches.
-template <int kVec, bool kOnce> __device__ __forceinline__ void copy_part(void *buffer, const Shape &s, int64_t src, int64_t dst, int32_t tokens, uint32_t part) {
+// Accesses [part * kThreads * kInFlight, ...) of the first `tokens` tokens of a page, on their way from one to others.  kOnce: read past the caches.
+template <int kVec, bool kOnce> struct Part {
   typedef typename Access<kVec>::any V;
-  const uint32_t outer = s.growing == 0 ? tokens : s.outer, middle = s.growing == 1 ? tokens : s.middle, inner = s.growing == 2 ? s.inner * tokens : s.inner;
-  const uint32_t each = (inner + kVec - 1) / kVec, n = outer * middle * each; // (fits: a page has fewer than 2^31 elements)
-  uint16_t *base = static_cast<uint16_t *>(buffer);
-  uint32_t at = part * (kThreads * kInFlight) + threadIdx.x;
   int64_t off[kInFlight];
   typename Access<kVec>::type v[kInFlight];
+  uint32_t at0, n;
+  __device__ __forceinline__ void load(const void *buffer, const Shape &s, int64_t page, int32_t tokens, uint32_t part) {
+    const uint32_t outer = s.growing == 0 ? tokens : s.outer, middle = s.growing == 1 ? tokens : s.middle, inner = s.growing == 2 ? s.inner * tokens : s.inner;
+    const uint32_t each = (inner + kVec - 1) / kVec;
+    n = outer * middle * each; // (fits: a page has fewer than 2^31 elements)
+    at0 = part * (kThreads * kInFlight) + threadIdx.x;
+    const uint16_t *base = static_cast<const uint16_t *>(buffer) + page * s.page;
 #pragma unroll
-  for (int k = 0; k < kInFlight; ++k, at += kThreads) {
-    if (at >= n) break;
-    const uint32_t run = at / each, x = min(at % each * kVec, inner - kVec);
-    off[k] = s.growing == 1 ? run / middle * s.outer_stride + run % middle * s.middle_stride + x : run * s.outer_stride + x;
-    const V *from = reinterpret_cast<const V *>(base + (src * s.page + off[k]));
-    v[k] = kOnce ? __builtin_nontemporal_load(from) : *from;
+    for (int k = 0; k < kInFlight; ++k) {
+      const uint32_t at = at0 + k * kThreads;
+      if (at >= n) break;
+      const uint32_t run = at / each, x = min(at % each * kVec, inner - kVec);
+      off[k] = s.growing == 1 ? run / middle * s.outer_stride + run % middle * s.middle_stride + x : run * s.outer_stride + x;
+      const V *from = reinterpret_cast<const V *>(base + off[k]);
+      v[k] = kOnce ? __builtin_nontemporal_load(from) : *from;
+    }
   }
-  at = part * (kThreads * kInFlight) + threadIdx.x;
+  __device__ __forceinline__ void store(void *buffer, const Shape &s, int64_t page) const {
+    uint16_t *base = static_cast<uint16_t *>(buffer) + page * s.page;
 #pragma unroll
-  for (int k = 0; k < kInFlight; ++k, at += kThreads) {
-    if (at >= n) break;
-    __builtin_nontemporal_store(v[k], reinterpret_cast<V *>(base + (dst * s.page + off[k])));
+    for (int k = 0; k < kInFlight; ++k) {
+      if (at0 + k * kThreads >= n) break;
+      __builtin_nontemporal_store(v[k], reinterpret_cast<V *>(base + off[k]));
+    }
   }
-}
+};
 
 // What moves: the first `tokens` tokens of a page, to another one.
 struct Move {
@@ -304,12 +311,24 @@ __device__ __forceinline__ void fork_rows(const Fork &f, int64_t wave, int64_t w
     if (threadIdx.x % kWave == 0) f.lens_out[r] = lost ? 0 : (int32_t)len;
   }
 }
+// Moves of a fork that a workgroup takes together.  us at 1 / 2 / 4 / 8: 16 prompts of up to 1000 tokens, 64 samples each in order, 32 layers of 8 heads (6.9 GB) 1940 / 1470 / 1288 / 1299, samples in
+// any order 1720 / 1720 / 1702 / 1726; 32 sequences into 128 in 160 buffers, in order, 57 / 59 / 61 / 63: as many moves as there are workgroups have nothing to gain.
+constexpr int kTogether = 4;
 // row_wgs: workgroups that write tables, a wavefront to a row; the others copy
 template <int kVec> __global__ __launch_bounds__(kThreads) void fork_apply(Fork f, Buffers buffers, Shape shape, uint32_t row_wgs, uint32_t parts) {
   if (blockIdx.x < row_wgs) return fork_rows(f, blockIdx.x * (int64_t)kWaves + threadIdx.x / kWave, (int64_t)row_wgs * kWaves);
-  each_part(min(f.totals[0], f.totals[1]), buffers.n, parts, blockIdx.x - row_wgs, gridDim.x - row_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
-    const Move m = f.moves[k];
-    copy_part<kVec, false>(buffers.at[b], shape, m.from, f.free_list[k], m.tokens, part); // (several may copy one page)
+  const int64_t moves = min(f.totals[0], f.totals[1]);
+  // Where there is enough to do, moves that follow one another are taken together, and read once if they are of one page (a prompt that goes on as many samples).
+  const int64_t together = moves * buffers.n * parts >= (int64_t)kTogether * (gridDim.x - row_wgs) ? kTogether : 1;
+  each_part((moves + together - 1) / together, buffers.n, parts, blockIdx.x - row_wgs, gridDim.x - row_wgs, [&](int64_t group, uint32_t b, uint32_t part) {
+    Part<kVec, false> data;
+    Move had = {-1, 0};
+    for (int64_t k = group * together; k < min(moves, (group + 1) * together); ++k) {
+      const Move m = f.moves[k];
+      if (m.from != had.from || m.tokens != had.tokens) data.load(buffers.at[b], shape, m.from, m.tokens, part);
+      had = m;
+      data.store(buffers.at[b], shape, f.free_list[k]);
+    }
   });
 }
 
@@ -712,7 +731,9 @@ template <int kVec> __global__ __launch_bounds__(kThreads) void compact_apply(Co
     return;
   }
   each_part(c.totals[0], buffers.n, parts, blockIdx.x - entry_wgs, gridDim.x - entry_wgs, [&](int64_t k, uint32_t b, uint32_t part) {
-    copy_part<kVec, true>(buffers.at[b], shape, c.from[k], c.to[k], page_tokens, part);
+    Part<kVec, true> data;
+    data.load(buffers.at[b], shape, c.from[k], page_tokens, part);
+    data.store(buffers.at[b], shape, c.to[k]);
   });
 }
 
@@ -750,7 +771,10 @@ template <typename F> hipError_t by_access(const Shape &s, int32_t page_tokens, 
   const uint32_t parts = (uint32_t)up(runs * up(inner, vec), kThreads * kInFlight);
   return vec == 8 ? f(std::integral_constant<int, 8>{}, parts) : f(std::integral_constant<int, 1>{}, parts);
 }
-constexpr int64_t kMostCopyWgs = 16384, kMostRowWgs = 2048;
+constexpr int64_t kMostRowWgs = 2048;
+// Workgroups that copy: how much there is to do only the GPU knows, and those that find nothing cost time too.  us at 4096 / 8192 / 16384: fork and compact as above 72.8 / 68.4-69.3 / 69.7 and
+// 199 / 191 / 184, 256 rows that go on as they are 9.6 / 11.5-13.5 / 15-19, 1024 pages in use and none to move 6.6 / 8.5 / 11.7.
+constexpr int64_t kMostForkWgs = 8192, kMostCompactWgs = 16384;
 // One workgroup keeps the books of up to kSoloPages pages and kSoloEntries entries of tables (of tables and slots, twice as many): us, by one / by launches after one another, fork of 256 rows of 8, 31
 // and 60 pages 8.8 / 16.1, 16.0 / 17.3, 25.5 / 17.8; grow by one token of 256 rows in 4096 and 16384 pages 8.0 / 10.2, 15.1 / 10.8, by 900 of 16 rows 10.5 / 12.6; compact of 1024, 8192 and 16384 pages
 // 7.5 / 13.7, 16.3 / 18.7, 26.9 / 23.8.
@@ -843,7 +867,7 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, void *stream) {
   const uint32_t row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
+    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostForkWgs);
     if (row_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(fork_apply<decltype(vec)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape, row_wgs, parts);
   });
@@ -876,7 +900,7 @@ int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, void *str
   const uint32_t entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
+    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCompactWgs);
     if (entry_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(compact_apply<decltype(vec)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape, pool.caches[0].page_tokens, entry_wgs, parts);
   });

@@ -146,7 +146,7 @@ def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, l
     prompt_lens[row] its prompt.  A token that is there: x / repetition[row] where x > 0, else x * repetition[row]; n times behind the prompt: less
     frequency[row] * n + presence[row] (all float32 [rows]).  bias_ids, bias [rows, places] (int32, float32): added to their tokens, of several the last; ids outside the vocabulary
     are left out.  allowed (int32 [masks, ceil(vocab / 32)], bit j % 32 of word j / 32): tokens whose bit is not set become -inf, by the mask
-    allowed_rows[row] (int32; outside the masks: none) or by the row's own.  out may be the logits; of rows without a mask then only what changes is written.  For
+    allowed_rows[row] (int32; outside the masks: none) or by the row's own.  out may be the logits; rows without a mask and with few tokens are then not moved.  For
     generation: it takes no gradient, and refuses tensors that require one where torch would take it."""
     return _steps.adjust(_stream_of(_device_of(logits)), logits, tokens, lens, prompt_lens, repetition, frequency, presence, bias_ids, bias, allowed, allowed_rows, out)
 

@@ -167,6 +167,29 @@ def test_adjust_infinities_and_nan(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("width", [900, 33000])
+@pytest.mark.parametrize("biases", [0, 20, 100])
+@pytest.mark.parametrize("dtype,tokens,vocab", [("bf16", torch.int64, 40001), ("f32", torch.int32, 40960), ("f16", torch.int64, 39999)])
+def test_adjust_few_tokens_in_place(dtype, tokens, vocab, biases, width):
+    """Rows of which little changes, beside one of which much does and one with a mask."""
+    from paper_2409_19256_amd import rollout
+    say("[adjust, in place]", dtype, biases, width)
+    gen = gen_of(dtype, biases, width)
+    x = logits_of(gen, 7, vocab, dtype, 1)
+    a = adjustment(dtype, 7, vocab, 0, width, tokens, biases, 2, gen)
+    a["lens"] = torch.tensor([0, 1, 63, 500, 880, width, 700], device="cuda", dtype=torch.int32)
+    a["prompt_lens"] = torch.tensor([0, 0, 30, 499, 1000, width // 2, -1], device="cuda", dtype=torch.int32)
+    a["allowed_rows"] = torch.tensor([-1, -1, 5, -1, 2, -1, 1], device="cuda", dtype=torch.int32)
+    got = rollout.adjust_logits(x, **a)
+    check_adjusted(got, x, a, dtype, "out of place")
+    store = torch.full((7, vocab + 3), 7.0, device="cuda", dtype=x.dtype)
+    mine = store[:, :vocab]
+    mine.copy_(x)
+    rollout.adjust_logits(mine, **a, out=mine)
+    assert torch.equal(bits_of(mine), bits_of(got)) and (store[:, vocab:] == 7).all()
+
+
+@pytest.mark.gpu
 def test_adjust_many_times_the_same_token():
     from paper_2409_19256_amd import rollout
     say("[adjust, 70000 times one token]")
