@@ -772,9 +772,9 @@ template <typename F> hipError_t by_access(const Shape &s, int32_t page_tokens, 
   return vec == 8 ? f(std::integral_constant<int, 8>{}, parts) : f(std::integral_constant<int, 1>{}, parts);
 }
 constexpr int64_t kMostRowWgs = 2048;
-// Workgroups that copy: how much there is to do only the GPU knows, and those that find nothing cost time too.  us at 4096 / 8192 / 16384: fork and compact as above 72.8 / 68.4-69.3 / 69.7 and
-// 199 / 191 / 184, 256 rows that go on as they are 9.6 / 11.5-13.5 / 15-19, 1024 pages in use and none to move 6.6 / 8.5 / 11.7.
-constexpr int64_t kMostForkWgs = 8192, kMostCompactWgs = 16384;
+// Workgroups that copy: how much there is to do only the GPU knows, and those that find nothing cost time too.  us at 4096 / 8192 / 16384: fork (call after call from Python) and compact as above
+// - / 73.5 / 71.0 and 199 / 191 / 184, 256 rows that go on as they are 9.6 / 11.5-13.5 / 15-19, 1024 pages in use and none to move 6.6 / 8.5 / 11.7.
+constexpr int64_t kMostCopyWgs = 16384;
 // One workgroup keeps the books of up to kSoloPages pages and kSoloEntries entries of tables (of tables and slots, twice as many): us, by one / by launches after one another, fork of 256 rows of 8, 31
 // and 60 pages 8.8 / 16.1, 16.0 / 17.3, 25.5 / 17.8; grow by one token of 256 rows in 4096 and 16384 pages 8.0 / 10.2, 15.1 / 10.8, by 900 of 16 rows 10.5 / 12.6; compact of 1024, 8192 and 16384 pages
 // 7.5 / 13.7, 16.3 / 18.7, 26.9 / 23.8.
@@ -867,7 +867,7 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, void *stream) {
   const uint32_t row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostForkWgs);
+    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostCopyWgs);
     if (row_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(fork_apply<decltype(vec)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape, row_wgs, parts);
   });
@@ -900,7 +900,7 @@ int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, void *str
   const uint32_t entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCompactWgs);
+    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
     if (entry_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(compact_apply<decltype(vec)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape, pool.caches[0].page_tokens, entry_wgs, parts);
   });
