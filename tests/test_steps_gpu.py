@@ -466,6 +466,32 @@ def test_fork(case, used):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out", [2000, 2100])
+@pytest.mark.parametrize("order", ["in order", "any"])
+def test_fork_into_many(out, order):
+    """So many copies that a workgroup takes several together: of one page, of pages that take turns, of one page to different lengths."""
+    say("[fork into many]", out, order)
+    gen = gen_of("many", out, order)
+    layers, pages, page = 40, 4200, 8
+    pool = new_pool(gen, layers, pages, 1, page, 8)
+    tables, lens, refs = sequences(gen, 20, 4, page, pages, used=0.02, full=0.1)
+    tables[3], lens[3] = tables[2], (lens[2] - 1).clamp(min=0)  # (against the rule: two that go on in one page)
+    parents = torch.randint(0, 20, (out,), generator=gen, device="cuda").int()
+    if order == "in order":
+        parents = parents.sort().values
+    want = S.fork(tables.cpu().numpy(), lens.cpu().numpy(), parents.cpu().numpy(), refs.cpu().numpy(), page)
+    assert len(want[3]) * 2 * layers > 4 * 16384
+    before = images(pool)
+    t, n, r = pool.fork(tables, lens, parents, refs)
+    same(t, want[0], "tables"), same(n, want[1], "lens"), same(r, want[2], "refs")
+    src, to, tokens = (torch.tensor(x, device="cuda") for x in zip(*want[3]))
+    moved = (torch.arange(page, device="cuda") < tokens[:, None])[:, None, :, None]
+    for x, old in zip(pool._tensors, before):
+        old[to] = torch.where(moved, old[src], old[to])
+        assert torch.equal(bits_of(x), bits_of(old))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("parents", ["same", "none", "one", "turned"])
 def test_fork_of_whole_batches(parents):
     say("[fork, all]", parents)
