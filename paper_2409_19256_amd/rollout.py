@@ -237,5 +237,7 @@ class PagePool:
                 refs_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
         """Moves pages so that the n in use are the first n.  Up to four tables (any shape) have their entries replaced.  Returns (tables, refs, places, n): where
         every page is now (int32, -1: free), and n (int32, no dimension).  tables_out may be tables."""
-        return _steps.compact(self._c, self._tensors, _stream_of(_device_of(refs)), refs, tuple(tables), tuple(tables_out) if tables_out is not None else (None,) * len(tables),
+        _need(not isinstance(tables, torch.Tensor) and not isinstance(tables_out, torch.Tensor), "tables: a list of tensors is wanted")
+        tables = tuple(tables)
+        return _steps.compact(self._c, self._tensors, _stream_of(_device_of(refs)), refs, tables, tuple(tables_out) if tables_out is not None else (None,) * len(tables),
                               refs_out, workspace)

@@ -100,6 +100,8 @@ refused(lambda: p.grow(t, one, one, T(5, dtype=i32), -1))
 refused(lambda: p.grow(t, one, one, T(5, dtype=i32), 2, slots=T(3, 3, dtype=i64)))
 refused(lambda: p.compact(T(5, dtype=i32), [t] * 5))
 refused(lambda: p.compact(T(5, dtype=i32), [t], [t, t]))
+refused(lambda: p.compact(T(5, dtype=i32), t), "list")
+refused(lambda: p.compact(T(5, dtype=i32), [t], t), "list")
 refused(lambda: p.compact(T(5, dtype=i32), [T(3, 4, dtype=i64)]))
 print("ok")
 """
