@@ -368,7 +368,7 @@ template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distil
 Logits logits_of(const hf_logits &in) { return {in.logits, in.row_stride, in.vocab, in.inv_temperature}; }
 
 // The forward pass reads plainly up to 512 MiB, so that the memory-side cache (256 MiB) keeps what it can for the gradient.  us, plain / non-temporal, forward and gradient of
-// 4096 x 32000 bf16 118 / 134, of 2048 x 128256 f32 533 / 529 (forward alone 197 / 179).
+// 4096 x 32000 bf16 118 / 134, of 2048 x 128256 f32 485 / 491, of 4096 x 128256 bf16 547 / 538; forward alone 178 / 163 and 185 / 167.  Rows in falling order for the gradient are level or up to 4 % behind.
 template <typename T, int kThreads> hipError_t launch_threads(const hf_logits &in, const hf_distillation &a, hipStream_t st) {
   const dim3 grid((uint32_t)in.rows);
   const bool once = in.rows * (int64_t)in.vocab * (int64_t)sizeof(T) > (int64_t)512 << 20;
