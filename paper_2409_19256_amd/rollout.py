@@ -195,7 +195,8 @@ class _Distill(torch.autograd.Function):
 
 def distill(logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, temperature: float = 1.0, reverse: float = 0.0,
             rest: bool = True) -> torch.Tensor:
-    """top_distill's loss of every row, differentiable with respect to the logits.  The teacher takes no gradient."""
+    """top_distill's loss of every row, differentiable with respect to the logits.  The teacher takes no gradient.  A backward pass is captured into a graph as torch's own
+    are: while no eager autograd graph of the same leaves is alive (torch would wait for its stream in the middle of the capture)."""
     _need(not (torch.is_grad_enabled() and isinstance(top_logprobs, torch.Tensor) and top_logprobs.requires_grad),
           "top_logprobs: no gradient is taken to the teacher: detach them")
     return _Distill.apply(logits, top_ids, top_logprobs, temperature, reverse, rest)
