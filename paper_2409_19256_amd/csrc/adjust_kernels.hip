@@ -195,7 +195,10 @@ template <typename T> hipError_t launch(const hf_adjustment &a, hipStream_t st) 
 
 } // namespace
 
-uint64_t adjust_wgs(const hf_adjustment &a) { return (uint64_t)a.rows * ((a.vocab + kChunk - 1) / kChunk); }
+bool adjust_fits(const hf_adjustment &a) {
+  constexpr uint64_t kMost = kMaxLanes / kThreads; // workgroups
+  return (uint64_t)a.rows <= kMost / ((a.vocab + kChunk - 1) / kChunk);
+}
 
 int launch_adjust(const hf_adjustment &a, void *stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -55,7 +55,8 @@ int launch_attend(const hf_kv_cache &cache, const hf_attention &args, const Atte
 int launch_token_logprobs(const hf_logits &in, const hf_logprobs &out, void *stream);
 int launch_token_logprobs_back(const hf_logits &in, const hf_logprobs_grad &grad, void *stream);
 
-constexpr uint64_t kMaxWgs = 0xFFFFFFFFull / 256; // a HIP grid holds fewer than 2^32 threads
+constexpr uint64_t kMaxLanes = 0xFFFFFFFFull;  // a HIP grid holds fewer than 2^32 threads
+constexpr uint64_t kMaxWgs = kMaxLanes / 256; // of 256 threads
 // workgroups per row of token_logprobs_back
 uint32_t logprob_back_segments(const hf_logits &in);
 

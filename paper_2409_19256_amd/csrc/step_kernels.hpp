@@ -5,12 +5,12 @@
 #include <cstdint>
 
 #include "hfreshard.h"
-#include "rollout_kernels.hpp" // enqueue_kernel, kMaxWgs
+#include "rollout_kernels.hpp" // enqueue_kernel, kMaxLanes, kMaxWgs
 
 namespace hf {
 
-// workgroups of adjust_logits
-uint64_t adjust_wgs(const hf_adjustment &args);
+// whether adjust_logits' workgroups fit a grid
+bool adjust_fits(const hf_adjustment &args);
 int launch_adjust(const hf_adjustment &args, void *stream);
 
 int launch_top_distill(const hf_logits &in, const hf_distillation &args, void *stream);

@@ -1,0 +1,22 @@
+"""Where the operators around a rollout's steps begin to refuse sizes, on both sides of every limit.  What is within one has to come to a later check, so that
+no call here runs: the operands overlap, or a pointer of the next check is missing."""
+import ctypes as C
+
+import pytest
+
+from paper_2409_19256_amd import binding as B
+from tests.test_rollout_refusals import AT
+from tests.test_steps_refusals import FAR, adjustment, run_adjust
+
+LANES = 1 << 32  # a grid holds fewer
+
+
+@pytest.mark.parametrize("vocab,pieces", [(32, 1), (8192, 1), (8193, 2), (128256, 16)])
+def test_adjustments_up_to_a_grid(vocab, pieces):
+    """Workgroups of 512 lanes, one to 8192 logits of a row."""
+    most = (LANES - 1) // 512 // pieces
+    bare = dict(vocab=vocab, row_stride=vocab, out_stride=vocab, tokens=None, lens=None, allowed=None, n_bias=0, repetition=None, frequency=None, presence=None, prompt_lens=None)
+    for rows, code in ((most, B.HF_EINVAL), (most + 1, B.HF_ERANGE), (2 * most, B.HF_ERANGE), (2 * most + 2, B.HF_ERANGE)):
+        a = adjustment(**bare, rows=rows, logits=FAR, out=FAR + 2)
+        assert run_adjust(a) == code, rows
+        assert (b"overlaps" if code == B.HF_EINVAL else b"too many rows") in B.hf_last_error(), rows
