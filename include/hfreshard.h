@@ -650,7 +650,8 @@ typedef struct {
   int32_t dtype;              /* HF_BF16, HF_F16 or HF_F32 */
   int32_t vocab;              /* 1 .. 2^30 */
   int32_t token_bytes;        /* 4 or 8 */
-  int32_t width, n_bias, n_allowed;
+  int32_t width, n_bias;      /* 0 .. 2^31 - 512 */
+  int32_t n_allowed;
 } hf_adjustment;
 HF_API int hf_adjust_logits(const hf_adjustment *args, void *hip_stream);
 

@@ -24,6 +24,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 512, kWave = 64;
 constexpr int kChunk = 8192; // logits of a piece
 constexpr int kHeld = 8;     // of a row's tokens that a lane keeps in registers
+static_assert((int64_t)kMaxAdjustList + kThreads <= (int64_t)INT32_MAX + 1, "a lane's place in a list, kThreads further at a time, stays in 32 bits");
 
 struct Row { // what one row's elements are changed by
   float rep, freq, pres;

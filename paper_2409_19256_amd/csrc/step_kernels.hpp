@@ -11,6 +11,7 @@ namespace hf {
 
 // whether adjust_logits' workgroups fit a grid
 bool adjust_fits(const hf_adjustment &args);
+constexpr int32_t kMaxAdjustList = INT32_MAX - 511; // tokens or biases of a row
 int launch_adjust(const hf_adjustment &args, void *stream);
 
 int launch_top_distill(const hf_logits &in, const hf_distillation &args, void *stream);

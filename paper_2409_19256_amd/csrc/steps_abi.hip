@@ -39,6 +39,7 @@ int check_adjustment(const hf_adjustment *p) {
   if (a.tokens && a.width && !span(tokens, a.width)) return set_error(HF_EINVAL, "tokens_stride is negative or spans too much");
   if (a.allowed && !span(allowed, words)) return set_error(HF_EINVAL, "allowed_stride is negative or spans too much");
   if (!separate(to, a.vocab)) return set_error(HF_EINVAL, "the output overlaps itself");
+  if (a.width > hf::kMaxAdjustList || a.n_bias > hf::kMaxAdjustList) return set_error(HF_ERANGE, "width and n_bias must be at most 2^31 - 512");
   if (!hf::adjust_fits(a)) return set_error(HF_ERANGE, "too many rows for one launch");
   const bool same = a.logits == a.out && (a.rows == 1 || a.row_stride == a.out_stride);
   const int64_t biases = a.n_bias > INT64_MAX / a.rows ? INT64_MAX : a.rows * a.n_bias;

@@ -20,3 +20,13 @@ def test_adjustments_up_to_a_grid(vocab, pieces):
         a = adjustment(**bare, rows=rows, logits=FAR, out=FAR + 2)
         assert run_adjust(a) == code, rows
         assert (b"overlaps" if code == B.HF_EINVAL else b"too many rows") in B.hf_last_error(), rows
+
+
+@pytest.mark.parametrize("what", ["width", "n_bias"])
+def test_adjustments_of_long_lists(what):
+    """Lanes go through lists in steps of 512, in numbers of 32 bits."""
+    most = (1 << 31) - 512
+    for n in (most - 1, most, most + 1, (1 << 31) - 1):
+        a = adjustment(**{what: n}, rows=1, tokens=FAR * 4, bias_ids=FAR * 8, bias=FAR * 16, out=AT + 2)
+        assert run_adjust(a) == (B.HF_ERANGE if n > most else B.HF_EINVAL), n
+        assert (b"2^31 - 512" if n > most else b"overlaps") in B.hf_last_error(), n
