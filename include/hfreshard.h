@@ -697,7 +697,7 @@ HF_API int hf_top_distill_back(const hf_logits *in, const hf_distillation_grad *
  * share pages that are full, one that is not belongs to one row.  The calls below read tables, lengths and reference counts on the device and write new ones, and move
  * whatever has to move in all caches, without a trip to the host.  Of a row's table the entries of its length count, cut to 0 .. width * page_tokens tokens; entries outside
  * 0 .. n_pages-1 name no page and come out as -1, and so do those behind.  Free pages are taken in rising order, so that results depend on the arguments alone.
- * refs_out may be refs; other outputs lie apart from inputs.  The workspace is 16-byte aligned, its contents do not matter and are not kept. */
+ * refs_out may be refs; other outputs lie apart from inputs, and all of them from the caches.  The workspace is 16-byte aligned, its contents do not matter and are not kept. */
 #define HF_MAX_CACHES 128
 typedef struct {
   const hf_kv_cache *caches; /* HOST memory: [n_caches] */

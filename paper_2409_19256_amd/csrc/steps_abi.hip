@@ -70,6 +70,14 @@ int check_pool(const hf_page_pool *p) {
 }
 
 // Keys and values of a pool's caches, as places in memory: all alike but for where they begin.
+Place first_of(const hf_page_pool &pool) {
+  const hf_kv_cache &c = pool.caches[0];
+  const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
+  Place p = place(c.k, dims, c.head_dim, 2);
+  for (const int i : {2, 1, 2}) // what of a page lies in one run is one run, so that an array of several tokens' size still has an exact answer
+    if (p.dims[i].n > 1 && p.dims[i].stride == p.inner) p.inner *= p.dims[i].n, p.dims[i] = {1, 0};
+  return p;
+}
 class Buffers {
   Place one_;
   uintptr_t begins_[2 * HF_MAX_CACHES]; // ascending
@@ -86,9 +94,7 @@ class Buffers {
 
 public:
   explicit Buffers(const hf_page_pool &pool) {
-    const hf_kv_cache &c = pool.caches[0];
-    const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
-    one_ = place(c.k, dims, c.head_dim, 2);
+    one_ = first_of(pool);
     for (int i = 0; i < pool.n_caches; ++i)
       for (const void *p : {pool.caches[i].k, pool.caches[i].v}) begins_[n_++] = reinterpret_cast<uintptr_t>(p);
     sort();
@@ -121,6 +127,23 @@ public:
     return false;
   }
 };
+
+// Whether an output of a call that leaves the caches alone lies in one of them.  Mostly all outputs are near one another and no cache is: one look at every buffer.
+template <size_t kN> bool in_a_cache(const hf_page_pool &pool, const Output (&outputs)[kN]) {
+  Place one = first_of(pool);
+  const uintptr_t size = one.end - one.begin;
+  uintptr_t begin = UINTPTR_MAX, end = 0;
+  for (const Output &o : outputs)
+    if (o.place.end) begin = std::min(begin, o.place.begin), end = std::max(end, o.place.end);
+  for (int i = 0; i < pool.n_caches; ++i)
+    for (const void *p : {pool.caches[i].k, pool.caches[i].v}) {
+      one.begin = reinterpret_cast<uintptr_t>(p), one.end = one.begin + size;
+      if (one.begin >= end || begin >= one.end) continue;
+      for (const Output &o : outputs)
+        if (overlap(one, o.place)) return true;
+    }
+  return false;
+}
 
 // a page in one buffer has to be countable in 32 bits
 int check_moves(const hf_page_pool &pool) {
@@ -275,6 +298,7 @@ int hf_grow_pages(const hf_page_pool *pool, const hf_page_grow *args, void *hip_
   // what is written where it was read meets no other output either
   if (const char *what = first_overlap(outputs, {a.tables == a.tables_out ? Place{} : tables, a.lens == a.lens_out ? Place{} : lens, counts, a.refs == a.refs_out ? Place{} : refs}))
     return set_error(HF_EINVAL, what);
+  if (in_a_cache(*pool, outputs)) return set_error(HF_EINVAL, "a cache overlaps an output");
   if (int rc = check_workspace(a.workspace, a.workspace_bytes, need)) return rc;
   return launched(hf::launch_grow(*pool, a, hip_stream));
 }
