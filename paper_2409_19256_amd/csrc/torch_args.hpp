@@ -86,11 +86,15 @@ struct Rows {
   for (PyObject *o : {keys, values})
     if (const Tensor &t = wanted(o, "cache"); !t.is_cuda() || t.get_device() != device) throw Wrong{"cache", "a cache on the operands' GPU is wanted"};
 }
-// The cache's operators have no backward: where torch would take a gradient they refuse, rather than lose it in silence.
+// Some operators have no backward: where torch would take a gradient they refuse, rather than lose it in silence; and so with the tangents of forward mode, which
+// no_grad does not end.
 [[maybe_unused]] void without_gradient(std::initializer_list<std::pair<const char *, const Tensor *>> tensors) {
-  if (!c10::GradMode::is_enabled()) return;
-  for (const auto &[name, t] : tensors)
-    if (t && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
+  const bool backward = c10::GradMode::is_enabled();
+  for (const auto &[name, t] : tensors) {
+    if (!t) continue;
+    if (backward && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
+    if (t->_fw_grad(0).defined()) throw Wrong{name, "no forward-mode gradient is taken here: unpack the dual tensor"};
+  }
 }
 // what a call has written to, for whoever saved it for a backward pass
 [[maybe_unused]] void written(std::initializer_list<const Tensor *> tensors) {

@@ -36,7 +36,7 @@ def _device_of(t) -> int:
 class KvCache:
     """Keys and values, each [page, KV head, token of the page, element] in any order of memory with the last contiguous
     (`KvCache.empty` makes one), for hf_append_kv and hf_attend.  Both are for generation and scoring: they take no gradient, and refuse
-    tensors that require one where torch would take it (call them under torch.no_grad())."""
+    tensors that require one where torch would take it (call them under torch.no_grad()), and dual tensors of forward mode."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         _need(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.is_cuda and k.device == v.device,
@@ -147,7 +147,7 @@ def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, l
     frequency[row] * n + presence[row] (all float32 [rows]).  bias_ids, bias [rows, places] (int32, float32): added to their tokens, of several the last; ids outside the vocabulary
     are left out.  allowed (int32 [masks, ceil(vocab / 32)], bit j % 32 of word j / 32): tokens whose bit is not set become -inf, by the mask
     allowed_rows[row] (int32; outside the masks: none) or by the row's own.  out may be the logits; rows without a mask and with few tokens are then not moved.  For
-    generation: it takes no gradient, and refuses tensors that require one where torch would take it."""
+    generation: it takes no gradient, and refuses tensors that require one where torch would take it, and dual tensors of forward mode."""
     return _steps.adjust(_stream_of(_device_of(logits)), logits, tokens, lens, prompt_lens, repetition, frequency, presence, bias_ids, bias, allowed, allowed_rows, out)
 
 
