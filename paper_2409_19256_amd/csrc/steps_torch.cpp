@@ -155,12 +155,13 @@ PyObject *distill(PyObject *, PyObject *const *arg, Py_ssize_t n_args) {
     const int rest = PyObject_IsTrue(arg[6]);
     if (rest < 0) throw python_error();
     a.flags = rest ? HF_DISTILL_REST : 0;
+    Tensor loss = at::empty({x.rows}, logits.options().dtype(at::kFloat)); // by itself: it outlives the step, and would hold the others
+    a.loss = static_cast<float *>(loss.data_ptr());
     Made made(logits);
-    const int loss = made.output(Py_None, "loss", at::kFloat, {x.rows}, &a.loss), norm = made.output(Py_None, "norm", at::kFloat, {x.rows, 2}, &a.norm);
-    const int slopes = made.output(Py_None, "slopes", at::kFloat, {x.rows, n + 1}, &a.slopes);
+    const int norm = made.output(Py_None, "norm", at::kFloat, {x.rows, 2}, &a.norm), slopes = made.output(Py_None, "slopes", at::kFloat, {x.rows, n + 1}, &a.slopes);
     made.make();
     if (const int code = hf_top_distill(&x, &a, stream_of(arg[0]))) return failed(code, "hf_top_distill");
-    return tuple_of({made.result(loss, Py_None), made.result(norm, Py_None), made.result(slopes, Py_None)});
+    return tuple_of({wrap(std::move(loss)), made.result(norm, Py_None), made.result(slopes, Py_None)});
   });
 }
 

@@ -152,7 +152,7 @@ def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, l
 
 
 class Distilled:
-    """What top_distill gives: loss [rows], and norm [rows, 2] and slopes [rows, places + 1] for top_distill_back."""
+    """What top_distill gives: loss [rows], and norm [rows, 2] and slopes [rows, places + 1] for top_distill_back.  The last two lie in one allocation, which either holds."""
     __slots__ = ("loss", "norm", "slopes")
 
     def __init__(self, loss, norm, slopes):
@@ -205,7 +205,9 @@ def distill(logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Ten
 class PagePool:
     """The pages of a model's caches (KvCache, one per layer, all alike): sequences are tables of page numbers (int32 [rows, width], as KvCache.attend takes
     them) with lengths in tokens (int32 [rows]), and refs (int32 [pages]) counts the rows that name a page; one with 0 is free.  Full pages may be shared, one that is not full
-    belongs to one row.  All calls run on the GPU without a trip to the host; what they return is new unless given (refs_out may be refs)."""
+    belongs to one row.  All calls run on the GPU without a trip to the host; what they return is new unless given (refs_out may be refs).
+    What one call returns anew lies in one allocation, with the call's workspace if that is small: each of these tensors holds all of it, torch.save writes all of it, and resize_ may
+    grow one over the next.  A tensor that is to outlive the others (compact's n, say) is cloned."""
 
     def __init__(self, caches: Sequence[KvCache]):
         _need(len(caches) > 0 and all(isinstance(c, KvCache) for c in caches), "at least one KvCache is wanted")
