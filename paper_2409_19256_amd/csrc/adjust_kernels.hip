@@ -12,6 +12,8 @@
 // take 33 / 27 / 26 and 254 / 210 / 245, so do 512 lanes for 4096 (35, 250) or 1024 for 8192 (35, 221).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "logit_rows.hpp"
 #include "step_kernels.hpp"
 
@@ -59,7 +61,7 @@ template <typename T> __device__ __forceinline__ uint32_t bits_of(const uint8_t 
   return kVec<T> == 8 ? allowed[v] : allowed[v / 2] >> (v % 2 * 4) & 15u;
 }
 
-template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __global__ __launch_bounds__(kThreads) void adjust_logits(hf_adjustment a, uint32_t pieces) {
+template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __global__ __launch_bounds__(kThreads) void adjust_logits(hf_adjustment a, uint32_t pieces, int32_t few) {
   constexpr int kV = kVec<T>, kPer = kChunk / kV / kThreads; // vectors of a lane
   typedef typename Vector<T>::type V;
   typedef Counts<kWide> C;
@@ -79,9 +81,8 @@ template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __gl
     if (g >= 0 && g < a.n_allowed) allowed = reinterpret_cast<const uint8_t *>(a.allowed + g * a.allowed_stride) + begin / 8;
   }
   const int n = kTables && a.tokens ? min(max(a.lens[r], 0), a.width) : 0;
-  // In place, without a mask and with few tokens nothing is moved but what changes.  us, by the token / by the piece, 1024 rows of 32000 bf16 with 64, 1024 and 4096 tokens 13.0 / 21.3, 20.4 / 23.8, 49.8 / 36.6,
-  // 1024 of 128256 f32 45 / 184, 72 / 194, 240 / 203: a token costs as much as some 40 logits.
-  const bool sparse = from == to && !allowed && n + (int64_t)a.n_bias <= a.vocab / 40;
+  // In place, without a mask and with few tokens nothing is moved but what changes.
+  const bool sparse = from == to && !allowed && n <= few;
   if (!kTables && sparse) return;
   const int n_last = sparse ? 0 : min(kV, size - n_vec * kV); // elements past the whole vectors, a lane each
 
@@ -181,17 +182,31 @@ template <typename T, typename Token, bool kTables, bool kWide, bool kMany> __gl
 
 // More biases than lanes of a wavefront are settled in a table of the piece, which leaves room for two workgroups on a CU instead of three.  us, a lane to a bias / by the table: 64 biases in 1024 rows of
 // 128256 f32 207 / 235, 16 in 64 rows of 32000 bf16 4.8 / 4.9.  Without the table (every bias against the others, 64 at a time): 300 in 4195 rows of 32000 f16 160 / 118, in 3 rows 8.7 / 4.7.
-template <typename T, typename Token, bool kWide> hipError_t launch_tables(const hf_adjustment &a, const dim3 &grid, uint32_t pieces, hipStream_t st) {
-  return enqueue_kernel(a.n_bias > kWave ? adjust_logits<T, Token, true, kWide, true> : adjust_logits<T, Token, true, kWide, false>, grid, kThreads, st, a, pieces);
+template <typename T, typename Token, bool kWide> hipError_t launch_tables(const hf_adjustment &a, const dim3 &grid, uint32_t pieces, int32_t few, hipStream_t st) {
+  return enqueue_kernel(a.n_bias > kWave ? adjust_logits<T, Token, true, kWide, true> : adjust_logits<T, Token, true, kWide, false>, grid, kThreads, st, a, pieces, few);
+}
+// Tokens up to which a row in place and without a mask is changed in memory, each by itself, beside its biases: one costs what moving 36 bytes of the row does, and as much as 1/3800 of the
+// row besides, since every piece goes through the whole list.  us, by the token / by the piece:
+//   tokens                64           512          1024         1536         2048         2560         4096       few: up to
+//   1024 x 32000 bf16   13.0 / 22.3  15.9 / 22.8  20.8 / 24.0  27.1 / 25.6  33.3 / 27.4  38.3 / 29.8  50.4 / 36.2     1230
+//   64 x 32000 bf16      3.3 / 4.0    3.7 / 4.2    4.2 / 4.5    5.0 / 4.7    5.4 / 5.0    5.9 / 5.3    7.7 / 6.2      1230
+//   4096 x 5004 f16     13.9 / 18.2  18.8 / 18.8  25.7 / 23.1  33.4 / 26.9  40.0 / 28.2  48.2 / 30.5  63.6 / 37.7      263
+//   1024 x 32000 f32    13.8 / 44.4  18.2 / 46.4  26.6 / 45.8  35.4 / 47.3  43.8 / 47.9  50.9 / 49.9  68.4 / 54.0     1855
+//   1024 x 128256 bf16  42.6 / 82.6  48.4 / 83.1  59.5 / 84.8  71.8 / 87.9  85.0 / 93.7  97.0 / 100    147 / 123      2490
+//   1024 x 128256 f32   45.8 / 169   54.2 / 174   71.7 / 171   89.1 / 170    112 / 172    144 / 177    242 / 183      3000
+template <typename T> int32_t few_tokens(const hf_adjustment &a) {
+  const int64_t row = a.vocab * (int64_t)sizeof(T);
+  return (int32_t)std::max<int64_t>(-1, row / (36 + row / 3800) - a.n_bias);
 }
 template <typename T> hipError_t launch(const hf_adjustment &a, hipStream_t st) {
   const uint32_t pieces = (a.vocab + kChunk - 1) / kChunk;
   const dim3 grid((uint32_t)(a.rows * pieces));
+  const int32_t few = few_tokens<T>(a);
   const bool text = a.tokens && a.width, wide = text && a.width >= 1 << 15;
-  if (text && a.token_bytes == 8) return wide ? launch_tables<T, int64_t, true>(a, grid, pieces, st) : launch_tables<T, int64_t, false>(a, grid, pieces, st);
-  if (text || a.n_bias) return wide ? launch_tables<T, int32_t, true>(a, grid, pieces, st) : launch_tables<T, int32_t, false>(a, grid, pieces, st);
+  if (text && a.token_bytes == 8) return wide ? launch_tables<T, int64_t, true>(a, grid, pieces, few, st) : launch_tables<T, int64_t, false>(a, grid, pieces, few, st);
+  if (text || a.n_bias) return wide ? launch_tables<T, int32_t, true>(a, grid, pieces, few, st) : launch_tables<T, int32_t, false>(a, grid, pieces, few, st);
   if (a.logits == a.out && !a.allowed) return hipSuccess;
-  return enqueue_kernel(adjust_logits<T, int32_t, false, false, false>, grid, kThreads, st, a, pieces);
+  return enqueue_kernel(adjust_logits<T, int32_t, false, false, false>, grid, kThreads, st, a, pieces, few);
 }
 
 } // namespace
