@@ -15,6 +15,8 @@
 // 64 bits on a chain (9.6 us forward for 1361 x 5004 f16, 7.4 for 64 x 32000 bf16).  Asking for the logits only when the list was known, and all wavefronts at the end, took 94 us for the 45.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
+
 #include "lanes.hpp"
 #include "logit_rows.hpp"
 #include "step_kernels.hpp"
@@ -103,7 +105,7 @@ template <typename T, int kThreads, int kPlaces, bool kOnce> __global__ __launch
   const int64_t r = blockIdx.x;
   const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, vocab = in.vocab;
   const T *row = static_cast<const T *>(in.data) + r * in.row_stride;
-  const float c = in.inv_temperature * kLog2e;
+  const float c = fminf(in.inv_temperature * kLog2e, FLT_MAX); // (times a difference of 0 it has to be 0)
 
   int32_t id = -1;
   float lq = 0;

@@ -208,3 +208,26 @@ def test_past_the_caches(dtype, vocab, places):
     loss, _, size_, *_ = S.distill(host(x[some]), ids[some].cpu().numpy(), host(lq[some]), 0.9, 0.5, True)
     rel = rel_of(dtype, vocab, 80)  # (a temperature that is rounded: u |D| more)
     near(host(whole[0][some]), loss, (2 * rel + 2 * U) * size_ + 2 * U * np.abs(loss), "loss")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("temperature", [3.5e-39, 2.0 ** -126, 2.0 ** 126, 2e38])
+@pytest.mark.parametrize("vocab", [1030, 131072 + 13])
+def test_the_ends_of_the_temperatures(vocab, temperature):
+    """Whatever 1 / temperature is in 32 bits: equal logits are equal, and others are nothing beside them or as good as equal."""
+    from paper_2409_19256_amd import rollout
+    say("[distill, temperatures]", vocab, temperature)
+    gen = gen_of("ends", vocab, temperature)
+    x = torch.full((3, vocab), 0.25, device="cuda")
+    x[1, 1::3] -= 1
+    x[2] = 3e38
+    ids = torch.arange(5, device="cuda", dtype=torch.int32).expand(3, 5) * 3  # among the largest
+    lq = QS.log().cuda().expand(3, 5).contiguous()
+    t = float(np.float32(1 / temperature)) ** -1  # what the kernel is given is exact
+    for reverse in (0.0, 1.0):
+        r = rollout.top_distill(x, ids.contiguous(), lq, t, reverse)
+        loss, _, size, *_ = by_logarithms(host(x), ids.cpu().numpy(), host(lq), t, reverse, True)
+        rel = rel_of("f32", vocab)
+        near(host(r.loss), loss, (2 * rel + 2 * U) * size + 2 * U * np.abs(loss), "loss")
+        grad = rollout.top_distill_back(x, ids.contiguous(), r.norm, r.slopes, torch.full((3,), min(1.0, t), device="cuda"), t)
+        assert torch.isfinite(grad).all()
