@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 
 #include "lanes.hpp"
 #include "logit_rows.hpp"
@@ -153,7 +154,7 @@ template <typename T, int kThreads, bool kTop> __global__ __launch_bounds__(kThr
   }
   const T *row = static_cast<const T *>(in.data) + r * in.row_stride;
   const float x_target = (float)row[target];
-  const float c = in.inv_temperature * kLog2e;
+  const float c = fminf(in.inv_temperature * kLog2e, FLT_MAX); // (times a difference of 0 it has to be 0)
   const int n_vec = vocab / kV; // whole ones
   Stats st = {-INFINITY, 0, 0, 0, 0};
   float limit = -INFINITY;
