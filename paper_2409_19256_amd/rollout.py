@@ -152,7 +152,8 @@ def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, l
 
 
 class Distilled:
-    """What top_distill gives: loss [rows], and norm [rows, 2] and slopes [rows, places + 1] for top_distill_back.  The last two lie in one allocation, which either holds."""
+    """What top_distill gives: loss [rows], and norm [rows, 2] and slopes [rows, places + 1] for top_distill_back.  The last two lie in one allocation, which either
+    holds; where all three are 4 KiB or less, the loss lies there too."""
     __slots__ = ("loss", "norm", "slopes")
 
     def __init__(self, loss, norm, slopes):

@@ -21,7 +21,8 @@ assert d.norm.untyped_storage().data_ptr() == d.slopes.untyped_storage().data_pt
 x = T(40, 500).requires_grad_()
 loss = R.distill(x, *lists)
 assert loss.requires_grad and held(loss) == held(loss.detach()) == 160
-assert held(R.top_distill(T(0, 500), T(0, 64, dtype=i32), T(0, 64, dtype=f32)).loss) == 0
+few = R.top_distill(T(3, 500), T(3, 64, dtype=i32), T(3, 64, dtype=f32)).loss  # (or a few numbers more)
+assert held(few) <= 4096 and R.top_distill(T(0, 500), T(0, 64, dtype=i32), T(0, 64, dtype=f32)).loss.shape == (0,)
 
 # tables, lengths and counts lie together, apart from one another
 p = R.PagePool([R.KvCache(T(5, 2, 4, 8), T(5, 2, 4, 8))])
