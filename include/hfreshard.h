@@ -638,7 +638,7 @@ HF_API int hf_token_logprobs_back(const hf_logits *in, const hf_logprobs_grad *g
 typedef struct {
   const void *logits;         /* [rows, vocab] of dtype */
   void *out;                  /* the same shape and type; may be the logits, with the same stride: rows without a mask and with few tokens are then not moved */
-  const void *tokens;         /* [rows, width] of int32 or int64; may be null */
+  const void *tokens;         /* [rows, width] of int32 or int64; may be null: then none is seen, and the penalties have nothing to apply to */
   const int32_t *lens;        /* [rows]; null exactly if tokens is */
   const int32_t *prompt_lens; /* [rows]; null: no prompts */
   const float *repetition, *frequency, *presence; /* [rows]; null: 1, 0 and 0 */
@@ -659,8 +659,9 @@ HF_API int hf_adjust_logits(const hf_adjustment *args, void *hip_stream);
 #define HF_DISTILL_REST 0x1u /* all tokens that are not named count together, as one more */
 /* hf_top_distill: how far rows of logits are from a teacher that is known by the log probabilities of some tokens (what hf_token_logprobs gives as
  * top_ids and top_logprobs, say).  p = softmax of y = x * inv_temperature; q_j = exp(logprobs[r, j]) and p_j belong to token ids[r, j].  With
- * HF_DISTILL_REST the other tokens are one more: p_rest is their sum, q_rest = max(0, 1 - sum q_j), whose logarithm is taken as that of 2^-24 at least.
+ * HF_DISTILL_REST the other tokens are one more: p_rest is their sum, q_rest = max(0, 1 - sum q_j).
  *   loss = (1 - reverse) sum q (log q - log p)  +  reverse sum p (log p - log q)
+ * In the second sum and its gradient log q_rest is taken as log 2^-24 at least, since p_rest stands before it; in the first it is itself, and the rest has no part in it where q_rest = 0.
  * A place of the list whose id is outside 0 .. vocab-1 or whose log probability is -inf names no token, and where an id comes twice its first place counts.  A row without any named
  * token has loss 0, whatever its logits are.  No rest is counted where no other token has p > 0 (all are named, or ruled out with -inf).  A named
  * token with x = -inf and q > 0 makes the loss inf if reverse < 1.  A row with NaN or +inf among its logits, or NaN among its log probabilities, has NaN results.
@@ -697,7 +698,8 @@ HF_API int hf_top_distill_back(const hf_logits *in, const hf_distillation_grad *
  * share pages that are full, one that is not belongs to one row.  The calls below read tables, lengths and reference counts on the device and write new ones, and move
  * whatever has to move in all caches, without a trip to the host.  Of a row's table the entries of its length count, cut to 0 .. width * page_tokens tokens; entries outside
  * 0 .. n_pages-1 name no page and come out as -1, and so do those behind.  Free pages are taken in rising order, so that results depend on the arguments alone.
- * refs_out may be refs; other outputs lie apart from inputs, and all of them from the caches.  The workspace is 16-byte aligned, its contents do not matter and are not kept. */
+ * refs_out may be refs; other outputs lie apart from inputs, and all of them from the caches.  The workspace is 16-byte aligned, its contents do not matter and are not kept; it is one
+ * call's until that has run. */
 #define HF_MAX_CACHES 128
 typedef struct {
   const hf_kv_cache *caches; /* HOST memory: [n_caches] */

@@ -7,8 +7,8 @@
 // is the token's last, or who is first to take the count away), and writes the piece.  The work beside the copy goes by the tokens and biases, not by the logits: a look at
 // every logit's count took more than HBM leaves room for.  In place, of rows without a mask and with few tokens, nothing is moved but what changes.
 //
-// us, out of place, beside the copy alone by the same workgroups: 1024 x 32000 bf16, 900 tokens a row, half of the rows masked 24.2 beside 22.0; 1024 x 128256 f32, 2800 tokens and 64 biases a row,
-// half masked 208 beside 170-189 (5.1 TB/s); 64 x 32000 bf16 4.8, one workgroup after another's data (lengths, tokens, counts, logits).  Pieces of 4096 / 8192 / 16384 (256 / 512 / 1024 lanes)
+// us, out of place, beside the copy alone by the same workgroups: 1024 x 32000 bf16, 900 tokens a row, half of the rows masked 24.7 beside 22.5; 1024 x 128256 f32, 2800 tokens and 64 biases a row,
+// half masked 194-208 beside 165-175 (5.1-5.4 TB/s); 64 x 32000 bf16 4.8, one workgroup after another's data (lengths, tokens, counts, logits).  Pieces of 4096 / 8192 / 16384 (256 / 512 / 1024 lanes)
 // take 33 / 27 / 26 and 254 / 210 / 245, so do 512 lanes for 4096 (35, 250) or 1024 for 8192 (35, 221).
 #include <hip/hip_runtime.h>
 

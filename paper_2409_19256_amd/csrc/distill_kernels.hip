@@ -10,9 +10,9 @@
 // difference of two sums.  Which are named stands in a bitmap in shared memory, a byte to a vector of 8.  The named tokens are a few numbers a row, taken in 64 bits
 // (a difference of logarithms near 1, one minus a sum of probabilities).  The gradient reads and writes every logit once; its named elements come out of a list.
 //
-// HBM is the bound of both where rows are many and long: forward 178 us (5.9 TB/s) and gradient 313 us (6.7 TB/s) of 2048 x 128256 f32, 45 and 59 us of 4096 x 32000 bf16 with a third of the rows left
-// out (3.9 and, partly from the memory-side cache, 7.4).  Short rows and few are bound by what follows one another: the list, the bitmap, the logits, joining wavefronts, and some twenty operations of
-// 64 bits on a chain (9.6 us forward for 1361 x 5004 f16, 7.4 for 64 x 32000 bf16).  Asking for the logits only when the list was known, and all wavefronts at the end, took 94 us for the 45.
+// HBM is the bound of both where rows are many and long: forward 160 us (6.6 TB/s) and gradient 333 us (6.3 TB/s) of 2048 x 128256 f32, 44 and 61 us of 4096 x 32000 bf16 with a third of the rows left
+// out (4.0 and, partly from the memory-side cache, 7.2).  Short rows and few are bound by what follows one another: the list, the bitmap, the logits, joining wavefronts, and some twenty operations of
+// 64 bits on a chain (10 us forward for 1361 x 5004 f16, 7.4 for 64 x 32000 bf16).  Asking for the logits only when the list was known, and all wavefronts at the end, took 94 us for the 44.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -312,7 +312,7 @@ constexpr int kBackThreads = 256;
 // A lane's vectors.  us at 1 / 2 / 4: 2048 x 128256 f32 383 / 348 / 387, 1361 x 5004 f32 14.0 / 11.6 / 13.7; of 16 bits two take 21 for the 16.5 of forward and gradient of 1361 x 5004.
 template <typename T> constexpr int kBackVectors = sizeof(T) == 4 ? 2 : 4;
 
-// A workgroup takes one of `segments` pieces of a row.  Both sides go past the caches: with plain stores (loads) 2048 x 128256 f32 forward and gradient take 592 (548) us for 529.
+// A workgroup takes one of `segments` pieces of a row.  Both sides go past the caches: with plain stores (loads) 2048 x 128256 f32 forward and gradient take 564 (510) us for 493.
 template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distill_back(Logits in, hf_distillation_grad g, uint32_t segments) {
   constexpr int kV = kVec<T>, kVectors = kBackVectors<T>, kPiece = kBackThreads * kVectors * kV;
   typedef typename Vector<T>::type V;
@@ -370,7 +370,7 @@ template <typename T> __global__ __launch_bounds__(kBackThreads) void top_distil
 Logits logits_of(const hf_logits &in) { return {in.logits, in.row_stride, in.vocab, in.inv_temperature}; }
 
 // The forward pass reads plainly up to 512 MiB, so that the memory-side cache (256 MiB) keeps what it can for the gradient.  us, plain / non-temporal, forward and gradient of
-// 4096 x 32000 bf16 118 / 134, of 2048 x 128256 f32 485 / 491, of 4096 x 128256 bf16 547 / 538; forward alone 178 / 163 and 185 / 167.  Rows in falling order for the gradient are level or up to 4 % behind.
+// 4096 x 32000 bf16 118 / 134, of 2048 x 128256 f32 486 / 493, of 4096 x 128256 bf16 549 / 541; forward alone 178 / 163 and 184 / 171.  Rows in falling order for the gradient are level or up to 4 % behind.
 template <typename T, int kThreads> hipError_t launch_threads(const hf_logits &in, const hf_distillation &a, hipStream_t st) {
   const dim3 grid((uint32_t)in.rows);
   const bool once = in.rows * (int64_t)in.vocab * (int64_t)sizeof(T) > (int64_t)512 << 20;

@@ -2,9 +2,9 @@
 //
 // First the books, then the data.  The books are reference counts and page tables: counts are changed by atomics (whole numbers, in any order the same), and what has an
 // order (the f-th free page to the f-th row that wants one) comes from sums over the rows and pages in front: of small batches by one workgroup with the counts in shared memory,
-// else over tiles, each tile's own in one launch and everybody's in the next.  The books are bound by what follows one another (one workgroup 2.5-4.5 us, the launches 12-16).  The data are copied by the next
+// else over tiles, each tile's own in one launch and everybody's in the next.  The books are bound by what follows one another (one workgroup 2.5-6 us, the launches 12-16).  The data are copied by the next
 // launch, which HBM bounds: 8 accesses of 16 bytes of a lane in flight, stores past the caches, the parts of a page on one XCD.  us of copying: a fork of 32 sequences into 128 in 160 buffers, 251 MB
-// written and 84 read, two thirds of them three times, 64 (5.2 TB/s); 245 pages of 512 KiB moved in four buffers, 1028 MB, 180 (5.7 TB/s).
+// written and, because three copies of a page are made by different workgroups, 182 read, 66-69 (6.4 TB/s); 245 pages of 512 KiB moved in four buffers, 1028 MB, 180 (5.7 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

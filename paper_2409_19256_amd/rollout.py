@@ -144,7 +144,7 @@ def adjust_logits(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, l
                   allowed: Optional[torch.Tensor] = None, allowed_rows: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Logits [rows, vocab] on their way to a choice of token.  tokens [rows, width] (int32 or int64) are what a row has so far, lens[row] of them (int32), the first
     prompt_lens[row] its prompt.  A token that is there: x / repetition[row] where x > 0, else x * repetition[row]; n times behind the prompt: less
-    frequency[row] * n + presence[row] (all float32 [rows]).  bias_ids, bias [rows, places] (int32, float32): added to their tokens, of several the last; ids outside the vocabulary
+    frequency[row] * n + presence[row] (all float32 [rows]); without tokens these have nothing to apply to.  bias_ids, bias [rows, places] (int32, float32): added to their tokens, of several the last; ids outside the vocabulary
     are left out.  allowed (int32 [masks, ceil(vocab / 32)], bit j % 32 of word j / 32): tokens whose bit is not set become -inf, by the mask
     allowed_rows[row] (int32; outside the masks: none) or by the row's own.  out may be the logits; rows without a mask and with few tokens are then not moved.  For
     generation: it takes no gradient, and refuses tensors that require one where torch would take it, and dual tensors of forward mode."""
