@@ -774,9 +774,9 @@ template <typename F> hipError_t by_access(const Shape &s, int32_t page_tokens, 
 constexpr int64_t kMostRowWgs = 2048;
 // Workgroups that copy: how much there is to do only the GPU knows, and those that find nothing cost time too.  us at 8192 / 10240 / 12288 / 16384, call after call from Python: rows that go on as they are, 256 of
 // them over 80 layers 13.7 / 15.0 / 16.5 / 19.2, 64 over 32 layers 12.4 / 13.5 / 14.9 / 17.7, 1024 over 20 layers 21.4 / 22.8 / 24.2 / 27.2; the fork as above 73.8 / 73.6 / 73.0 / 71.0 (replayed from a graph
-// 69.1 / 70.5 / 69.6 / 69.5), 16 prompts into 64 samples each over 8 layers of 8 heads 339 / 335 / 334 / 331.  Most steps of a rollout fork rows that go on as they are.  Compact as above at 4096 / 8192 / 16384 199 / 191 / 184,
-// 1024 pages in use and none to move 6.6 / 8.5 / 11.7.
-constexpr int64_t kMostForkWgs = 8192, kMostCompactWgs = 16384;
+// 69.1 / 70.5 / 69.6 / 69.5).  Most steps of a rollout fork rows that go on as they are.  Where more rows come out than went in, some branch: 16 prompts into 64 samples each over 8 layers of 8 heads
+// 339 / 335 / 334 / 331.  Compact as above at 4096 / 8192 / 16384 199 / 191 / 184, 1024 pages in use and none to move 6.6 / 8.5 / 11.7.
+constexpr int64_t kMostCopyWgs = 16384, kMostForkWgs = 8192;
 // One workgroup keeps the books of up to kSoloPages pages and kSoloEntries entries of tables (of tables and slots, twice as many): us, by one / by launches after one another, fork of 256 rows of 8, 31
 // and 60 pages 8.8 / 16.1, 16.0 / 17.3, 25.5 / 17.8; grow by one token of 256 rows in 4096 and 16384 pages 8.0 / 10.2, 15.1 / 10.8, by 900 of 16 rows 10.5 / 12.6; compact of 1024, 8192 and 16384 pages
 // 7.5 / 13.7, 16.3 / 18.7, 26.9 / 23.8.
@@ -869,7 +869,7 @@ int launch_fork(const hf_page_pool &pool, const hf_page_fork &a, void *stream) {
   const uint32_t row_wgs = solo ? 0 : wgs(a.rows_out, kWaves).x;
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, kMostForkWgs);
+    const int64_t copies = std::min((int64_t)a.rows_out * 2 * pool.n_caches * parts, a.rows_out > a.rows ? kMostCopyWgs : kMostForkWgs);
     if (row_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(fork_apply<decltype(vec)::value>, dim3(row_wgs + (uint32_t)copies), kThreads, st, f, buffers_of(pool), shape, row_wgs, parts);
   });
@@ -902,7 +902,7 @@ int launch_compact(const hf_page_pool &pool, const hf_page_compact &a, void *str
   const uint32_t entry_wgs = (uint32_t)std::min(up(most, kThreads), kMostRowWgs);
   const Shape shape = shape_of(pool.caches[0]);
   return by_access(shape, pool.caches[0].page_tokens, [&](auto vec, uint32_t parts) {
-    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCompactWgs);
+    const int64_t copies = std::min((int64_t)c.n_pages / 2 * 2 * pool.n_caches * parts, kMostCopyWgs);
     if (entry_wgs + copies == 0) return hipSuccess;
     return enqueue_kernel(compact_apply<decltype(vec)::value>, dim3(entry_wgs + (uint32_t)copies), kThreads, st, c, buffers_of(pool), shape, pool.caches[0].page_tokens, entry_wgs, parts);
   });
