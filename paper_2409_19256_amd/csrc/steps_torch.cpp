@@ -212,9 +212,10 @@ struct Pool {
   }
   // the GPU that all tensors are on has to be the pool's; `moves`: data are written, which takes no gradient
   void check(int device, bool moves) const {
+    const Modes modes; // looked at once for all of them
     each([&](const Tensor &t) {
       if (!t.is_cuda() || t.get_device() != device) throw Wrong{"pool", "caches on the operands' GPU are wanted"};
-      if (moves) without_gradient({{"pool", &t}});
+      if (moves) without_gradient({{"pool", &t}}, modes);
     });
   }
   void moved() const {

@@ -8,6 +8,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -86,14 +87,17 @@ struct Rows {
   for (PyObject *o : {keys, values})
     if (const Tensor &t = wanted(o, "cache"); !t.is_cuda() || t.get_device() != device) throw Wrong{"cache", "a cache on the operands' GPU is wanted"};
 }
-// Some operators have no backward: where torch would take a gradient they refuse, rather than lose it in silence; and so with the tangents of forward mode, which
-// no_grad does not end.
-[[maybe_unused]] void without_gradient(std::initializer_list<std::pair<const char *, const Tensor *>> tensors) {
-  const bool backward = c10::GradMode::is_enabled();
+// What torch would take a gradient by: backward, and forward mode, whose tangents live as long as its level and which no_grad does not end.
+struct Modes {
+  bool backward = c10::GradMode::is_enabled(), forward = torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr;
+};
+// Some operators have no gradient: where torch would take one they refuse, rather than lose it in silence.
+[[maybe_unused]] void without_gradient(std::initializer_list<std::pair<const char *, const Tensor *>> tensors, const Modes &modes = Modes()) {
+  if (!modes.backward && !modes.forward) return;
   for (const auto &[name, t] : tensors) {
     if (!t) continue;
-    if (backward && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
-    if (t->_fw_grad(0).defined()) throw Wrong{name, "no forward-mode gradient is taken here: unpack the dual tensor"};
+    if (modes.backward && t->requires_grad()) throw Wrong{name, "no gradient is taken here: detach it, or call under torch.no_grad()"};
+    if (modes.forward && t->_fw_grad(0).defined()) throw Wrong{name, "no forward-mode gradient is taken here: unpack the dual tensor"};
   }
 }
 // what a call has written to, for whoever saved it for a backward pass
