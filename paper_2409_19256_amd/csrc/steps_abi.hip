@@ -69,7 +69,7 @@ int check_pool(const hf_page_pool *p) {
   return HF_OK;
 }
 
-// Keys and values of a pool's caches, as places in memory: all alike but for where they begin.
+// The first cache's keys, as a place in memory.
 Place first_of(const hf_page_pool &pool) {
   const hf_kv_cache &c = pool.caches[0];
   const Dim dims[] = {{c.n_pages, c.page_stride}, {c.n_kv_heads, c.head_stride}, {c.page_tokens, c.token_stride}};
@@ -78,6 +78,8 @@ Place first_of(const hf_page_pool &pool) {
     if (p.dims[i].n > 1 && p.dims[i].stride == p.inner) p.inner *= p.dims[i].n, p.dims[i] = {1, 0};
   return p;
 }
+
+// Keys and values of a pool's caches, as places in memory: all alike but for where they begin.
 class Buffers {
   Place one_;
   uintptr_t begins_[2 * HF_MAX_CACHES]; // ascending
